@@ -441,6 +441,139 @@ typedef struct netmax_shape {
 } netmax_shape;
 int netmax_launch_shape(netmax_ctx* ctx, int64_t n_rounds, netmax_shape* out);
 
+/*
+ * ---- Operators on real weights ---------------------------------------------------------------------
+ *
+ * A replica may hold the weights of a model.  These calls compute a layer and its gradient for every worker with that worker's
+ * own weights, orthogonalise updates, and take the local step and the pull of a round from given gradients.
+ *
+ * All arrays are device memory of `storage`'s type (momentum: fp32 in both).  A netmax_view names M matrices: element (r, c) of
+ * worker i is data[i * worker_stride + r * row_stride + c], strides in elements.  Inputs may overlap and repeat (worker_stride = 0
+ * gives every worker the same matrix); the matrices of an output must not overlap each other or any input, except
+ * that y may be the residual itself (the same address and strides).  Elements that no view names are left as they are.
+ * Products are summed in fp32.  fp32 operands enter them as two fp16 parts scaled by a power of two per matrix (22 bits below the
+ * matrix's largest finite magnitude); bfloat16 operands enter as they are.  Every other step is fp32, rounded once when it is
+ * stored.  An infinity or NaN among the inputs makes the outputs that depend on it infinite or NaN.
+ *
+ * `workspace` is device memory, 256-byte aligned, of the size that the matching call returns.  Calls that share one must run one
+ * after the other (two captured graphs that share one, too).  Nothing is allocated and nothing waits for the device, so all of these
+ * can be captured in a graph.  Every wait inside the kernels is bounded; netmax_workspace_status says whether one ran out.
+ */
+typedef struct netmax_view {
+  void* data;            /* device; not written where the view is an input */
+  int64_t row_stride;
+  int64_t worker_stride;
+} netmax_view;
+
+enum { NETMAX_ACTIVATION_NONE = 0, NETMAX_ACTIVATION_RELU = 1, NETMAX_ACTIVATION_GELU = 2, NETMAX_ACTIVATION_SILU = 3 };
+
+/* A layer of M workers: z = x W^T + bias, y = act(z) + residual, for n rows (n >= 0; n * n_in, n * n_out and n_in * n_out < 2^31).
+ * gelu is z Phi(z), silu z / (1 + exp(-z)). */
+typedef struct netmax_layer {
+  int32_t M;
+  int64_t n, n_in, n_out;
+  int32_t storage;
+  int32_t activation;
+  netmax_view x;         /* n x n_in                                                                     */
+  netmax_view weight;    /* n_out x n_in                                                                 */
+  netmax_view bias;      /* 1 x n_out; data NULL: none                                                   */
+  netmax_view residual;  /* n x n_out; data NULL: none (forward)                                         */
+  netmax_view y;         /* n x n_out, written (forward)                                                 */
+  netmax_view z;         /* n x n_out: written by forward unless data is NULL; read by backward, which needs it
+                            with an activation                                                           */
+  netmax_view dy;        /* n x n_out (backward)                                                         */
+  netmax_view dx;        /* n x n_in, written (backward); data NULL: not wanted                          */
+  netmax_view dweight;   /* n_out x n_in, written (backward); data NULL: not wanted                      */
+  netmax_view dbias;     /* 1 x n_out, written (backward); data NULL: not wanted                         */
+  int32_t device;
+  void* stream;
+  void* workspace;
+  size_t workspace_bytes;
+} netmax_layer;
+int netmax_layer_workspace_size(int32_t M, int64_t n, int64_t n_in, int64_t n_out, int32_t storage, size_t* bytes);
+int netmax_layer_forward(const netmax_layer* layer);
+/* dz = dy act'(z); dx = dz W; dweight = dz^T x; dbias = the sums of dz over the rows.  The gradient of the residual is dy. */
+int netmax_layer_backward(const netmax_layer* layer);
+
+/*
+ * Orthogonalises every matrix u: X = u / |u| (Frobenius), then `steps` times X <- a X + b (X X^T) X + c (X X^T)^2 X with
+ * (a, b, c) = (3.4445, -4.7750, 2.0315): the singular values go to about 1 (between 0.68 and 1.21 after five steps for
+ * values from 0.002 |u| on), the singular vectors stay.  A matrix of zeros gives zeros; one with an infinity or NaN gives NaN everywhere.
+ * Iterates carry 22 bits; with fp32 storage the products do, too, with bfloat16 storage their factors are rounded to fp16 (11 bits).
+ */
+typedef struct netmax_orthogonal {
+  int32_t count;
+  int64_t rows, cols;    /* rows * cols < 2^31 */
+  int32_t storage;
+  int32_t steps;         /* 1 ... 20 */
+  netmax_view u;         /* worker_stride: from one matrix to the next */
+  netmax_view out;
+  int32_t device;
+  void* stream;
+  void* workspace;
+  size_t workspace_bytes;
+} netmax_orthogonal;
+int netmax_orthogonalise_workspace_size(int32_t count, int64_t rows, int64_t cols, int32_t storage, size_t* bytes);
+int netmax_orthogonalise(const netmax_orthogonal* o);
+
+/* A matrix inside a replica: `rows` rows of `cols` elements from `offset` on, without gaps. */
+typedef struct netmax_matrix {
+  int64_t offset, rows, cols;
+  double scale;          /* factor of its orthogonalised update */
+} netmax_matrix;
+
+/*
+ * One update of all workers from given gradients g:
+ *   m' = mu m + g;  u = g + mu m' (nesterov) or m';  o = scale * orthogonalised(u) inside the matrices, u elsewhere;
+ *   h_i = x_i - lr (o_i + decay x_i)     (Eq. 15 with o for the gradient)
+ *   x_i' = h_i - w_i (h_i - x_m)         (Eq. 16 with the peer m = peers[i]; h_i where m = i, or m is no worker)
+ * Replicas, gradients and momentum are M rows of d elements.  momentum_next may be momentum; x_next overlaps nothing else.
+ */
+typedef struct netmax_step {
+  int32_t M;
+  int64_t d;
+  int32_t storage;
+  netmax_view x, x_next, gradient;            /* row_stride is not read */
+  netmax_view momentum, momentum_next;        /* fp32; row_stride is not read */
+  const netmax_matrix* matrices;              /* host; at most 256, of at most 2^31 - 1 elements, none overlapping another */
+  int32_t n_matrices;
+  const int32_t* peers;                       /* device, M */
+  const float* weights;                       /* device, M */
+  double lr, mu, decay;                       /* used at their fp32 roundings */
+  int32_t nesterov;
+  int32_t steps;
+  int32_t device;
+  void* stream;
+  void* workspace;
+  size_t workspace_bytes;
+} netmax_step;
+int netmax_orthogonalised_step_workspace_size(int32_t M, int64_t d, const netmax_matrix* matrices, int32_t n_matrices, int32_t storage, size_t* bytes);
+int netmax_orthogonalised_step(const netmax_step* step);
+
+/*
+ * A synchronous round of a context from given gradients: like netmax_round(1) -- the same peer draws and pull weights, the same
+ * trace and telemetry (on the replicas before the round, the loss against the centres) --, with netmax_orthogonalised_step in
+ * the place of the quadratic objective's step.  lr is the context's.
+ */
+typedef struct netmax_update {
+  const void* gradient;       /* device, M rows of d elements of the context's storage type */
+  int64_t gradient_stride;    /* elements from one worker's to the next's */
+  float* momentum;            /* device, M rows of d fp32, updated in place */
+  int64_t momentum_stride;
+  const netmax_matrix* matrices;
+  int32_t n_matrices;
+  double mu, decay;
+  int32_t nesterov;
+  int32_t steps;
+  void* workspace;            /* of netmax_orthogonalised_step_workspace_size */
+  size_t workspace_bytes;
+} netmax_update;
+int netmax_round_orthogonalised(netmax_ctx* ctx, const netmax_update* update);
+
+/* Waits for `stream` and returns NETMAX_CUDA_ERROR if a bounded wait ran out in the last call that used `workspace` (its outputs
+ * are then not to be used). */
+int netmax_workspace_status(const void* workspace, int32_t device, void* stream);
+
 /* Counters for benchmarks: kernels launched by this context so far. */
 int64_t netmax_kernel_launches(const netmax_ctx* ctx);
 

@@ -28,6 +28,9 @@ EXPORTS = [
     "netmax_measure", "netmax_async_begin", "netmax_async_set_times", "netmax_async_steps", "netmax_async_time",
     "netmax_async_trace", "netmax_async_ema", "netmax_async_monitor", "netmax_async_monitor_refreshes",
     "netmax_iteration_times", "netmax_policy_generate", "netmax_policy_generate_ex", "netmax_policy_generate_device", "netmax_policy_generate_fixed_weight", "netmax_policy_fixed_weight_at", "netmax_debug_absent_ctas", "netmax_launch_shape", "netmax_kernel_launches", "netmax_last_error",
+    "netmax_layer_workspace_size", "netmax_layer_forward", "netmax_layer_backward", "netmax_orthogonalise_workspace_size",
+    "netmax_orthogonalise", "netmax_orthogonalised_step_workspace_size", "netmax_orthogonalised_step",
+    "netmax_round_orthogonalised", "netmax_workspace_status",
 ]
 
 
@@ -51,6 +54,42 @@ class Shape(C.Structure):
     _fields_ = [("kernel", C.c_int32), ("groups", C.c_int32), ("rows", C.c_int32), ("warps", C.c_int32), ("own_instance", C.c_int32)]
 
 
+class View(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("worker_stride", C.c_int64)]
+
+
+class Layer(C.Structure):
+    _fields_ = [("M", C.c_int32), ("n", C.c_int64), ("n_in", C.c_int64), ("n_out", C.c_int64), ("storage", C.c_int32),
+                ("activation", C.c_int32), ("x", View), ("weight", View), ("bias", View), ("residual", View), ("y", View), ("z", View),
+                ("dy", View), ("dx", View), ("dweight", View), ("dbias", View), ("device", C.c_int32), ("stream", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class Orthogonal(C.Structure):
+    _fields_ = [("count", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64), ("storage", C.c_int32), ("steps", C.c_int32),
+                ("u", View), ("out", View), ("device", C.c_int32), ("stream", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
+class Matrix(C.Structure):
+    _fields_ = [("offset", C.c_int64), ("rows", C.c_int64), ("cols", C.c_int64), ("scale", C.c_double)]
+
+
+class Step(C.Structure):
+    _fields_ = [("M", C.c_int32), ("d", C.c_int64), ("storage", C.c_int32), ("x", View), ("x_next", View), ("gradient", View),
+                ("momentum", View), ("momentum_next", View), ("matrices", C.c_void_p), ("n_matrices", C.c_int32), ("peers", C.c_void_p),
+                ("weights", C.c_void_p), ("lr", C.c_double), ("mu", C.c_double), ("decay", C.c_double), ("nesterov", C.c_int32),
+                ("steps", C.c_int32), ("device", C.c_int32), ("stream", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
+class Update(C.Structure):
+    _fields_ = [("gradient", C.c_void_p), ("gradient_stride", C.c_int64), ("momentum", C.c_void_p), ("momentum_stride", C.c_int64),
+                ("matrices", C.c_void_p), ("n_matrices", C.c_int32), ("mu", C.c_double), ("decay", C.c_double), ("nesterov", C.c_int32),
+                ("steps", C.c_int32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 KERNELS = ("round", "multi_round", "fused", "tiles", "pipe")
 STORAGE = {"f32": 0, "bf16": 1}
 
@@ -112,6 +151,15 @@ def lib():
             "netmax_launch_shape": ([vp, i64, vp], C.c_int),
             "netmax_kernel_launches": ([vp], i64),
             "netmax_last_error": ([vp], C.c_char_p),
+            "netmax_layer_workspace_size": ([i32, i64, i64, i64, i32, vp], C.c_int),
+            "netmax_layer_forward": ([vp], C.c_int),
+            "netmax_layer_backward": ([vp], C.c_int),
+            "netmax_orthogonalise_workspace_size": ([i32, i64, i64, i32, vp], C.c_int),
+            "netmax_orthogonalise": ([vp], C.c_int),
+            "netmax_orthogonalised_step_workspace_size": ([i32, i64, vp, i32, i32, vp], C.c_int),
+            "netmax_orthogonalised_step": ([vp], C.c_int),
+            "netmax_round_orthogonalised": ([vp, vp], C.c_int),
+            "netmax_workspace_status": ([vp, i32, vp], C.c_int),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -195,6 +243,139 @@ def netmax_policy_generate_device(t_iter, adj, lr: float, K: int, R: int, device
     return P, rho.value, dict(lam2=info[0], tbar=info[1], t_conv=info[2], k=int(info[3]), r=int(info[4]))
 
 
+# ---- operators on real weights: device arrays are torch tensors (or anything with data_ptr, shape, stride, dtype and device)
+_NO_VIEW = View(None, 0, 0)
+
+
+def _storage_of(t):
+    kind = {"torch.float32": 0, "torch.bfloat16": 1}.get(str(t.dtype))
+    if kind is None:
+        raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
+    return kind
+
+
+def _view(name, t, like, shape):
+    """A device tensor as a netmax_view: of `like`'s type and device, of this shape (M, rows, cols) or (M, cols), columns contiguous."""
+    if t is None:
+        return _NO_VIEW
+    if t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name}: expected {like.dtype} on {like.device}, got {t.dtype} on {t.device}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    rows, cols = (shape[1], shape[2]) if len(shape) == 3 else (1, shape[1])
+    row = strides[1] if rows > 1 else cols
+    return View(t.data_ptr(), row, strides[0] if shape[0] > 1 else max(1, rows) * row)
+
+
+def _device_of(t):
+    if t.device.type != "cuda":
+        raise ValueError(f"expected a CUDA tensor, got one on {t.device}")
+    return t.device.index or 0
+
+
+def _workspace(t, like):
+    if t is None:
+        return None, 0
+    if t.device != like.device:
+        raise ValueError(f"workspace: expected {like.device}, got {t.device}")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def netmax_layer_workspace_size(M: int, n: int, n_in: int, n_out: int, storage: str = "f32") -> int:
+    out = C.c_size_t()
+    _check(lib().netmax_layer_workspace_size(int(M), int(n), int(n_in), int(n_out), STORAGE[storage], C.byref(out)))
+    return out.value
+
+
+def netmax_layer_forward(x, weight, y, bias=None, residual=None, z=None, activation: str = "none", workspace=None,
+                         stream: Optional[int] = None):
+    """y = act(x W^T + bias) + residual for every worker; z, if given, gets the pre-activation.  x (M, n, n_in), weight
+    (M, n_out, n_in), bias (M, n_out), residual, y and z (M, n, n_out), all of one type."""
+    M, n, n_in = x.shape
+    n_out = weight.shape[1]
+    ws, size = _workspace(workspace, x)
+    rows = (M, n, n_out)
+    a = Layer(M, n, n_in, n_out, _storage_of(x), ACTIVATIONS[activation], _view("x", x, x, (M, n, n_in)),
+              _view("weight", weight, x, (M, n_out, n_in)), _view("bias", bias, x, (M, n_out)), _view("residual", residual, x, rows),
+              _view("y", y, x, rows), _view("z", z, x, rows), _NO_VIEW, _NO_VIEW, _NO_VIEW, _NO_VIEW, _device_of(x), stream, ws, size)
+    code = lib().netmax_layer_forward(C.addressof(a))
+    if code:
+        _check(code)
+
+
+def netmax_layer_backward(dy, x, weight, dx=None, dweight=None, dbias=None, z=None, activation: str = "none", workspace=None,
+                          stream: Optional[int] = None):
+    """The gradient of netmax_layer_forward: whichever of dx, dweight and dbias are given are written.  z: what forward wrote there."""
+    M, n, n_out = dy.shape
+    n_in = weight.shape[2]
+    ws, size = _workspace(workspace, dy)
+    a = Layer(M, n, n_in, n_out, _storage_of(dy), ACTIVATIONS[activation], _view("x", x, dy, (M, n, n_in)),
+              _view("weight", weight, dy, (M, n_out, n_in)), _NO_VIEW, _NO_VIEW, _NO_VIEW, _view("z", z, dy, (M, n, n_out)),
+              _view("dy", dy, dy, (M, n, n_out)), _view("dx", dx, dy, (M, n, n_in)), _view("dweight", dweight, dy, (M, n_out, n_in)),
+              _view("dbias", dbias, dy, (M, n_out)), _device_of(dy), stream, ws, size)
+    code = lib().netmax_layer_backward(C.addressof(a))
+    if code:
+        _check(code)
+
+
+def netmax_orthogonalise_workspace_size(count: int, rows: int, cols: int, storage: str = "f32") -> int:
+    out = C.c_size_t()
+    _check(lib().netmax_orthogonalise_workspace_size(int(count), int(rows), int(cols), STORAGE[storage], C.byref(out)))
+    return out.value
+
+
+def netmax_orthogonalise(u, out, steps: int = 5, workspace=None, stream: Optional[int] = None):
+    """Every matrix of u (count, rows, cols) orthogonalised by Newton-Schulz steps, into out."""
+    count, rows, cols = u.shape
+    ws, size = _workspace(workspace, u)
+    a = Orthogonal(count, rows, cols, _storage_of(u), int(steps), _view("u", u, u, (count, rows, cols)),
+                   _view("out", out, u, (count, rows, cols)), _device_of(u), stream, ws, size)
+    code = lib().netmax_orthogonalise(C.addressof(a))
+    if code:
+        _check(code)
+
+
+def matrix_table(matrices):
+    """[(offset, rows, cols, scale)] as the table that the steps take; a program makes it once."""
+    if isinstance(matrices, C.Array):
+        return matrices
+    return (Matrix * len(matrices))(*[Matrix(int(o), int(r), int(c), float(s)) for o, r, c, s in matrices])
+
+
+def netmax_orthogonalised_step_workspace_size(M: int, d: int, matrices, storage: str = "f32") -> int:
+    table, out = matrix_table(matrices), C.c_size_t()
+    _check(lib().netmax_orthogonalised_step_workspace_size(int(M), int(d), C.addressof(table), len(table), STORAGE[storage], C.byref(out)))
+    return out.value
+
+
+def netmax_orthogonalised_step(x, x_next, gradient, momentum, momentum_next, matrices, peers, weights, lr: float, mu: float = 0.95,
+                               nesterov: bool = True, decay: float = 0.0, steps: int = 5, workspace=None, stream: Optional[int] = None):
+    """One update of all workers: x, x_next, gradient (M, d) of one type, momentum (M, d) float32, peers (M,) int32, weights (M,) float32."""
+    M, d = x.shape
+    table = matrix_table(matrices)
+    for name, t, kind in (("momentum", momentum, "torch.float32"), ("peers", peers, "torch.int32"), ("weights", weights, "torch.float32")):
+        if str(t.dtype) != kind or t.device != x.device:
+            raise ValueError(f"{name}: expected {kind} on {x.device}, got {t.dtype} on {t.device}")
+    if tuple(peers.shape) != (M,) or tuple(weights.shape) != (M,) or not peers.is_contiguous() or not weights.is_contiguous():
+        raise ValueError(f"peers and weights: expected {M} contiguous elements each")
+    ws, size = _workspace(workspace, x)
+    a = Step(M, d, _storage_of(x), _view("x", x, x, (M, d)), _view("x_next", x_next, x, (M, d)), _view("gradient", gradient, x, (M, d)),
+             _view("momentum", momentum, momentum, (M, d)), _view("momentum_next", momentum_next, momentum, (M, d)), C.addressof(table),
+             len(table), peers.data_ptr(), weights.data_ptr(), float(lr), float(mu), float(decay), int(bool(nesterov)), int(steps),
+             _device_of(x), stream, ws, size)
+    code = lib().netmax_orthogonalised_step(C.addressof(a))
+    if code:
+        _check(code)
+
+
+def netmax_workspace_status(workspace, stream: Optional[int] = None):
+    """Waits for the stream; raises if a bounded wait ran out in the last call that used this workspace."""
+    _check(lib().netmax_workspace_status(workspace.data_ptr(), _device_of(workspace), stream))
+
+
 class Netmax:
     """One simulator context (netmax_create_ex ... netmax_destroy)."""
 
@@ -226,7 +407,7 @@ class Netmax:
         cfg.first_round = int(first_round)
         self.first_round = int(first_round)
         self.storage = storage
-        self.M, self.d = int(M), int(d)
+        self.M, self.d, self.device = int(M), int(d), int(device)
         self._h = C.c_void_p()
         self._L = L
         _check(L.netmax_create_ex(C.byref(cfg), C.byref(self._h)))
@@ -373,6 +554,23 @@ class Netmax:
         cons, loss = C.c_double(), C.c_double()
         _check(lib().netmax_measure(self._h, C.byref(cons), C.byref(loss)), self._h)
         return cons.value, loss.value
+
+    def round_orthogonalised(self, gradient, momentum, matrices, mu: float = 0.95, nesterov: bool = True, decay: float = 0.0,
+                             steps: int = 5, workspace=None):
+        """netmax_round_orthogonalised: gradient (M, d) of the storage type and momentum (M, d) float32 are device tensors."""
+        table = matrix_table(matrices)
+        if _storage_of(gradient) != STORAGE[self.storage]:
+            raise ValueError(f"gradient: expected {self.storage} values, got {gradient.dtype}")
+        if str(momentum.dtype) != "torch.float32" or momentum.device != gradient.device:
+            raise ValueError(f"momentum: expected torch.float32 on {gradient.device}, got {momentum.dtype} on {momentum.device}")
+        if _device_of(gradient) != self.device:
+            raise ValueError(f"gradient: expected a tensor on device {self.device}, got one on {gradient.device}")
+        g = _view("gradient", gradient, gradient, (self.M, self.d))
+        m = _view("momentum", momentum, momentum, (self.M, self.d))
+        ws, size = _workspace(workspace, gradient)
+        a = Update(g.data, g.worker_stride, m.data, m.worker_stride, C.addressof(table), len(table), float(mu), float(decay),
+                   int(bool(nesterov)), int(steps), ws, size)
+        _check(self._L.netmax_round_orthogonalised(self._h, C.addressof(a)), self._h)
 
     # ---- asynchronous timeline (one worker per global step)
     def async_begin(self, t_iter=None, beta: float = 0.9):

@@ -23,6 +23,7 @@
 
 #include "netmax_plain.cuh"
 #include "netmax_instances.h"
+#include "netmax_operators.h"
 #include "netmax_policy.h"
 
 using namespace netmax;
@@ -1899,6 +1900,72 @@ int netmax_round(netmax_ctx* ctx, int64_t n_rounds) try {
   return NETMAX_OK;
 } NM_CATCH_CTX(ctx)
 
+// (consensus, loss) of the current replicas, by the measuring instantiation of the round kernel; `plan` is plan_round's for it.
+static int launch_measure(netmax_ctx* ctx, const RoundPlan& plan, double* out) {
+  RoundParams p = make_round_params(ctx, plan);
+  p.x_cur = reinterpret_cast<const float4*>(ctx->x[ctx->cur]);
+  p.tel_out = out;
+  RoundKernel kernel = pick_kernel(2, plan.short_vectors, ctx->L.halves);
+  kernel<<<plan.grid, kThreads, plan.smem, ctx->stream>>>(p);
+  ctx->launches += 1;
+  NM_CUDA(ctx, cudaGetLastError());
+  return NETMAX_OK;
+}
+
+int netmax_round_orthogonalised(netmax_ctx* ctx, const netmax_update* update) try {
+  if (!ctx) return fail(nullptr, NETMAX_INVALID_ARG, "ctx is NULL");
+  if (!update) return fail(ctx, NETMAX_INVALID_ARG, "update is NULL");
+  if (ctx->async_on) return fail(ctx, NETMAX_INVALID_ARG, "the context runs the asynchronous timeline; use netmax_async_steps");
+  if ((uint64_t)(ctx->rounds + 1) >= ((uint64_t)1 << 56)) return fail(ctx, NETMAX_INVALID_ARG, "round counter would exceed 2^56");
+  const int64_t slot = ctx->rounds % ctx->trace_rounds;
+  const int2* draws = ctx->draws + slot * ctx->M;
+  netmax_step t;
+  std::memset(&t, 0, sizeof t);
+  t.M = ctx->M;
+  t.d = ctx->d;
+  t.storage = ctx->storage;
+  t.x = {ctx->x[ctx->cur], ctx->L.ld, ctx->L.ld};
+  t.x_next = {ctx->x[ctx->cur ^ 1], ctx->L.ld, ctx->L.ld};
+  t.gradient = {const_cast<void*>(update->gradient), ctx->d, update->gradient_stride};
+  t.momentum = t.momentum_next = {update->momentum, ctx->d, update->momentum_stride};
+  t.matrices = update->matrices;
+  t.n_matrices = update->n_matrices;
+  t.peers = &draws->x;
+  t.weights = reinterpret_cast<const float*>(&draws->y);
+  t.lr = ctx->alpha;
+  t.mu = update->mu;
+  t.decay = update->decay;
+  t.nesterov = update->nesterov;
+  t.steps = update->steps;
+  t.device = ctx->device;
+  t.stream = ctx->stream;
+  t.workspace = update->workspace;
+  t.workspace_bytes = update->workspace_bytes;
+  auto noted = [&](int code) {  // (the operators' messages belong to no context)
+    if (code) ctx->error = g_error;
+    return code;
+  };
+  int rc = noted(check_step(t));
+  if (rc) return rc;
+  DeviceGuard guard(ctx->device);
+  RoundPlan plan;
+  rc = plan_round(ctx, plan, 2);
+  if (rc) return rc;
+  ctx->host_writes = true;
+  ctx->staged = false;
+  choose_rings(ctx, 1);
+  rc = launch_sampler(ctx, (uint64_t)ctx->rounds, 1, ctx->trace, ctx->draws, slot, ctx->trace_rounds);
+  if (rc) return rc;
+  rc = launch_measure(ctx, plan, ctx->tel + 2 * slot);
+  if (rc) return rc;
+  rc = noted(enqueue_step(t, 2, const_cast<unsigned int*>(ctx->dev_error), &ctx->launches));
+  if (rc) return rc;
+  ctx->cur ^= 1;
+  ctx->rounds += 1;
+  ctx->read_since_round = false;
+  return NETMAX_OK;
+} NM_CATCH_CTX(ctx)
+
 int64_t netmax_rounds_done(const netmax_ctx* ctx) { return ctx ? ctx->rounds : -1; }
 
 // ---- host round trip, pipelined over column chunks ----------------------------------------------
@@ -2204,35 +2271,9 @@ int netmax_measure(netmax_ctx* ctx, double* consensus, double* loss) {
   RoundPlan plan;
   int rc = plan_round(ctx, plan, 2);  // 2: the measuring instantiation of the round kernel
   if (rc) return rc;
-  RoundKernel kernel = pick_kernel(2, plan.short_vectors, ctx->L.halves);
-  RoundParams p;
-  std::memset(&p, 0, sizeof p);
-  p.x_cur = reinterpret_cast<const float4*>(ctx->x[ctx->cur]);
-  p.x_nxt = nullptr;
-  p.c = reinterpret_cast<const float4*>(ctx->c);
-  p.peers = nullptr;
-  p.wtab = ctx->wtab;
-  p.partials = ctx->partials;
-  p.ticket = ctx->ticket;
-  p.tel_out = ctx->measure_out;
-  p.ldq = ctx->L.ldq;
-  p.row_bytes = (uint32_t)(ctx->L.ld * ctx->L.elem);
-  p.nq = ctx->L.nq;
-  p.n_tiles = plan.n_tiles;
-  p.M = ctx->M;
-  p.tail = (int32_t)(ctx->d % (4 * ctx->L.halves));
-  p.cg = plan.cg;
-  p.rl = plan.rl;
-  p.rg = plan.rg;
-  p.rows_per_group = plan.rows_per_group;
-  p.colpart = ctx->colpart;
-  p.coltick = ctx->coltick;
-  p.inv_M = 1.0f / (float)ctx->M;
-  p.keys = ctx->keys;
   ctx->host_writes = true;
-  kernel<<<plan.grid, kThreads, plan.smem, ctx->stream>>>(p);
-  ctx->launches += 1;
-  NM_CUDA(ctx, cudaGetLastError());
+  rc = launch_measure(ctx, plan, ctx->measure_out);
+  if (rc) return rc;
   rc = synchronise(ctx);
   if (consensus) *consensus = ctx->measure_out[0];
   if (loss) *loss = ctx->measure_out[1];

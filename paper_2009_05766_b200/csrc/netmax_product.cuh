@@ -1,0 +1,584 @@
+// Batched matrix products on the tensor cores (tcgen05, accumulators in TMEM, operands by TMA), one kernel for all of the
+// operators that train real weights in the replicas.
+//
+//   D[m][n] = sum_k A[m][k] B[n][k]        m = the output's contiguous dimension, n = its rows
+//
+// Both operands are 16-bit (fp16 or bf16) and lie in memory either with k contiguous or with m (n) contiguous; the descriptors of the
+// tensor cores and the order of the TMA coordinates say which, so no operand is ever transposed.  fp32 operands come as two
+// fp16 planes, hi = fp16(s v) and lo = fp16(s v - hi) with s a power of two: 22 bits, so that
+//   hi hi + hi lo + lo hi = s^2 A B^T (1 + O(2^-22))
+// costs three products in one accumulator instead of one (the term lo lo is below the fp32 accumulator's own rounding).
+//
+// One CTA pair (cta_group::2) works on a tile of 256 x up to 256, each CTA with its own 128 rows of A and half the rows of B in
+// shared memory: a tile of k = 64 then costs an SM 32 KB from L2 for 512 cycles of tensor work, 48 KB if every CTA worked for
+// itself.  Problems that would leave SMs without a tile that way take one CTA per tile of 128 x 64 to 128 x 256.  Warps 0-7 are the
+// epilogue, warp 8 issues the TMA loads, warp 9 the products; the accumulators are double-buffered so that the epilogue of a tile
+// runs under the products of the next.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+namespace netmax {
+
+constexpr int kProductThreads = 320;      // eight epilogue warps, one that loads, one that multiplies
+constexpr int kProductBox = 64;           // a TMA box: 64 rows of 64 16-bit values (128 bytes, the swizzle's width)
+constexpr int kBoxBytes = kProductBox * 128;
+constexpr int kMaxGroups = 12;            // groups of equal matrices in one launch
+constexpr int kMaxMatrices = 256;         // matrices of one replica in one launch
+constexpr int kMaxStages = 8;
+constexpr float kPlaneScale = 16384.0f;   // 2^14: what the planes of Newton-Schulz iterates are scaled by (all |v| < 2.9)
+constexpr float kPlaneUnscale = 1.0f / 16384.0f;
+
+enum { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
+enum Epilogue {
+  kLayerF32, kLayerBf16,  // y = act(D + bias) + residual, z = D + bias
+  kGram,                  // planes of D (symmetric)
+  kPolynomial,            // planes of b A + c D (symmetric), A from planes
+  kUpdate,                // planes of a X + D, X from planes
+  kLastF32, kLastBf16,    // the same, out as fp32 / bf16
+  kStepF32, kStepBf16,    // the same, into a worker's local step and its pull
+};
+
+struct ProductGroup {
+  CUtensorMap a, b;  // {contiguous, other, matrix, plane}
+  int32_t tile_begin = 0, tiles_m = 0, tiles_n = 0;
+  int32_t M = 0, N = 0, K = 0;
+  int32_t symmetric = 0;       // tiles on and below the diagonal, the others mirrored
+  int32_t a_mn = 0, b_mn = 0;  // m (n) contiguous instead of k
+  int32_t bn = 0;              // columns of a tile
+  int32_t a_batched = 1, b_batched = 1;  // 0: one matrix for all
+  uint32_t idesc = 0;
+  // epilogue: element (n, m) of matrix q at base + q * batch + n * row + m
+  void* out = nullptr;
+  int64_t out_row = 0, out_batch = 0, out_plane = 0;
+  void* z = nullptr;
+  int64_t z_row = 0, z_batch = 0;
+  const void* bias = nullptr;
+  int64_t bias_batch = 0;
+  const void* residual = nullptr;  // or the planes of A (kPolynomial) and X (kUpdate, kLast*, kStep*)
+  int64_t residual_row = 0, residual_batch = 0, residual_plane = 0;
+  int32_t activation = 0;
+  const int32_t *exp_a = nullptr, *exp_b = nullptr;  // per matrix: its planes hold 2^exp times the values
+  int32_t first_matrix = 0;                          // of the step's table
+};
+
+struct PullParams {  // a worker's local step and pull, behind the last product
+  const void* x = nullptr;
+  void* x_next = nullptr;
+  int64_t x_row = 0, next_row = 0;
+  const int32_t* peers = nullptr;
+  const float* weights = nullptr;
+  int32_t draw_stride = 1;  // peers[draw_stride i] and weights[draw_stride i] are worker i's
+  float lr = 0, decay = 0;
+  int32_t workers = 0;
+};
+
+struct ProductParams {
+  ProductGroup group[kMaxGroups];
+  PullParams step;
+  uint32_t matrix_offset[kMaxMatrices];
+  float matrix_scale[kMaxMatrices];
+  int32_t groups = 0, tiles = 0, planes = 1, stages = 2;
+  uint32_t stage_bytes = 0, a_bytes = 0, b_bytes = 0;  // of a stage; of one plane of A and of B in it
+  float ca = 0, cb = 0, cc = 0;        // the quintic's coefficients
+  unsigned int* error = nullptr;       // raised by a wait that ran out
+  int32_t clear_error = 0;
+};
+
+// ---- the few instructions that have no CUDA C++ form ------------------------------------------
+namespace ptx {
+__device__ __forceinline__ uint32_t smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ bool elect() {
+  uint32_t pred;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(pred));
+  return pred != 0;
+}
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void expect_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {  // bar: an address of the cluster's window
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ uint32_t map_to(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0;
+}
+__device__ __forceinline__ uint64_t now_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+// False if the phase did not end within two seconds (or 2^26 looks, whichever comes first).
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
+  for (int i = 0; i < 64; ++i)
+    if (try_wait(bar, parity)) return true;
+  const uint64_t start = now_ns();
+  for (uint32_t i = 0; i < (1u << 26); ++i) {
+    if (try_wait(bar, parity)) return true;
+    if ((i & 255) == 255 && now_ns() - start > 2000000000ull) return false;
+  }
+  return false;
+}
+template <int kCtas>
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
+  if (kCtas == 2)
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+template <int kCtas>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  if (kCtas == 2)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+// Arrives at `bar` (in both CTAs of a pair) when every product issued so far has been done.
+template <int kCtas>
+__device__ __forceinline__ void commit(uint32_t bar) {
+  if (kCtas == 2)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+template <int kCtas>
+__device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t columns) {
+  if (kCtas == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+}
+template <int kCtas>
+__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t columns) {
+  if (kCtas == 2)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
+  else
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
+}
+__device__ __forceinline__ void tmem_load32(uint32_t at, float (&v)[32]) {
+  uint32_t r[32];
+  __syncwarp();
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, "
+      "%20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(at));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void wait_for_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_successor_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// Shared-memory descriptor of an operand tile in 128-byte swizzled rows.  k contiguous: groups of eight rows are 1024 bytes apart.
+// m (n) contiguous: a row is 64 values of one k; groups of eight k are 1024 bytes apart, blocks of 64 m a box apart.
+__device__ __forceinline__ uint64_t descriptor(uint32_t at, bool mn) {
+  const uint64_t leading = mn ? kBoxBytes >> 4 : 1;
+  return (uint64_t)((at & 0x3FFFF) >> 4) | leading << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+}  // namespace ptx
+
+__device__ __forceinline__ float activate(float z, int activation) {
+  if (activation == kActRelu) return z > 0.0f ? z : (z != z ? z : 0.0f);
+  if (activation == kActGelu) return 0.5f * z * erfcf(z * -0.70710678118654752f);
+  if (activation == kActSilu) return z / (1.0f + expf(-z));
+  return z;
+}
+__device__ __forceinline__ float activation_slope(float z, int activation) {
+  if (activation == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
+  if (activation == kActGelu) return 0.5f * erfcf(z * -0.70710678118654752f) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+  const float s = 1.0f / (1.0f + expf(-z));
+  return s * (1.0f + z * (1.0f - s));
+}
+// v 2^e in two factors, so that neither overflows or loses bits where the result does not.
+__device__ __forceinline__ float scale_by_power(float v, int e) {
+  const int half = e / 2;
+  return ldexpf(1.0f, half) * v * ldexpf(1.0f, e - half);
+}
+// The two fp16 planes of a scaled value; what is not finite stays so, once.
+__device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
+  hi = __float2half_rn(v);
+  const float h = __half2float(hi);
+  lo = fabsf(h) <= 65504.0f ? __float2half_rn(v - h) : __float2half_rn(0.0f);
+}
+
+__device__ __forceinline__ uint32_t pack2(__half a, __half b) { return (uint32_t)__half_as_ushort(a) | (uint32_t)__half_as_ushort(b) << 16; }
+__device__ __forceinline__ uint4 pack8(const __half* h) { return make_uint4(pack2(h[0], h[1]), pack2(h[2], h[3]), pack2(h[4], h[5]), pack2(h[6], h[7])); }
+
+struct Tile {
+  int g, q, i, j;  // group, matrix, tile row (m) and column (n)
+};
+__device__ __forceinline__ Tile find_tile(const ProductParams& p, int t) {
+  Tile r;
+  r.g = 0;
+  while (r.g + 1 < p.groups && p.group[r.g + 1].tile_begin <= t) ++r.g;
+  const ProductGroup& g = p.group[r.g];
+  t -= g.tile_begin;
+  if (g.symmetric) {
+    const int per = g.tiles_m * (g.tiles_m + 1) / 2;
+    r.q = t / per;
+    t -= r.q * per;
+    int i = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);  // (at most one off: i is small)
+    while (i * (i + 1) / 2 > t) --i;
+    while ((i + 1) * (i + 2) / 2 <= t) ++i;
+    r.i = i;
+    r.j = t - i * (i + 1) / 2;
+  } else {
+    const int per = g.tiles_m * g.tiles_n;
+    r.q = t / per;
+    t -= r.q * per;
+    r.j = t / g.tiles_m;
+    r.i = t - r.j * g.tiles_m;
+  }
+  return r;
+}
+
+// 32 columns of one row m of the accumulator: element (n0 + c, m) for c = 0 ... 31.
+template <int kEpilogue>
+__device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const ProductGroup& g, const Tile& t, int m, int n0, int exponent, float (&v)[32]) {
+  if (m >= g.M) return;
+  const int count = min(32, g.N - n0);  // (the same for the whole warp)
+  if (kEpilogue == kLayerF32 || kEpilogue == kLayerBf16) {
+    using T = typename std::conditional<kEpilogue == kLayerF32, float, __nv_bfloat16>::type;
+    const float bias = g.bias ? (float)((const T*)g.bias)[t.q * g.bias_batch + m] : 0.0f;
+    const T* r = g.residual ? (const T*)g.residual + t.q * g.residual_batch + n0 * g.residual_row + m : nullptr;
+    T* z = g.z ? (T*)g.z + t.q * g.z_batch + n0 * g.z_row + m : nullptr;
+    T* y = (T*)g.out + t.q * g.out_batch + n0 * g.out_row + m;
+#pragma unroll
+    for (int c0 = 0; c0 < 32; c0 += 8) {
+      if (c0 >= count) break;
+      float add[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) add[c] = r && c0 + c < count ? (float)r[(c0 + c) * g.residual_row] : 0.0f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        if (c0 + c >= count) break;
+        float s = v[c0 + c];
+        if (kEpilogue == kLayerF32) s = scale_by_power(s, exponent);
+        s += bias;
+        if (z) z[(c0 + c) * g.z_row] = (T)s;
+        s = activate(s, g.activation);
+        if (r) s += add[c];
+        y[(c0 + c) * g.out_row] = (T)s;
+      }
+    }
+    return;
+  }
+  if (kEpilogue == kGram || kEpilogue == kPolynomial) {
+    const bool two = p.planes == 2;
+    const int64_t at = t.q * g.out_batch + (int64_t)n0 * g.out_row + m;
+    __half before[2][32];
+    if (kEpilogue == kPolynomial) {
+      const __half* a = (const __half*)g.residual + t.q * g.residual_batch + (int64_t)n0 * g.residual_row + m;
+#pragma unroll
+      for (int c = 0; c < 32; ++c) {
+        before[0][c] = c < count ? a[c * g.residual_row] : __half(0.0f);
+        before[1][c] = two && c < count ? a[c * g.residual_row + g.residual_plane] : __half(0.0f);
+      }
+    }
+    __half* out = (__half*)g.out;
+    __half hi[32], lo[32];
+#pragma unroll
+    for (int c = 0; c < 32; ++c) {
+      float s = v[c] * kPlaneUnscale;
+      if (kEpilogue == kPolynomial) s = p.cb * (__half2float(before[0][c]) + __half2float(before[1][c])) + p.cc * s;
+      split(s, hi[c], lo[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < 32; ++c) {
+      if (c >= count) break;
+      out[at + c * g.out_row] = hi[c];
+      if (two) out[at + c * g.out_row + g.out_plane] = lo[c];
+    }
+    if (t.i != t.j) {  // the mirrored half: this thread's columns are contiguous there
+      __half* mirror = out + t.q * g.out_batch + (int64_t)m * g.out_row + n0;
+      if (count == 32) {
+#pragma unroll
+        for (int c = 0; c < 32; c += 8) *(uint4*)(mirror + c) = pack8(hi + c);
+        if (two) {
+#pragma unroll
+          for (int c = 0; c < 32; c += 8) *(uint4*)(mirror + g.out_plane + c) = pack8(lo + c);
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          if (c >= count) break;
+          mirror[c] = hi[c];
+          if (two) mirror[g.out_plane + c] = lo[c];
+        }
+      }
+    }
+    return;
+  }
+  // a X + D: X always comes in two planes (fp32's accuracy), whatever the products take
+  __half x[2][32];
+  const __half* a = (const __half*)g.residual + t.q * g.residual_batch + (int64_t)n0 * g.residual_row + m;
+#pragma unroll
+  for (int c = 0; c < 32; ++c) {
+    x[0][c] = c < count ? a[c * g.residual_row] : __half(0.0f);
+    x[1][c] = c < count ? a[c * g.residual_row + g.residual_plane] : __half(0.0f);
+  }
+#pragma unroll
+  for (int c = 0; c < 32; ++c) v[c] = p.ca * (__half2float(x[0][c]) + __half2float(x[1][c])) + v[c] * kPlaneUnscale;
+  if (kEpilogue == kUpdate) {
+    __half* out = (__half*)g.out + t.q * g.out_batch + (int64_t)n0 * g.out_row + m;
+#pragma unroll
+    for (int c = 0; c < 32; ++c) {
+      if (c >= count) break;
+      __half hi, lo;
+      split(v[c], hi, lo);
+      out[c * g.out_row] = hi;
+      out[c * g.out_row + g.out_plane] = lo;
+    }
+  } else if (kEpilogue == kLastF32 || kEpilogue == kLastBf16) {
+    using T = typename std::conditional<kEpilogue == kLastF32, float, __nv_bfloat16>::type;
+    T* out = (T*)g.out + t.q * g.out_batch + (int64_t)n0 * g.out_row + m;
+#pragma unroll
+    for (int c = 0; c < 32; ++c) {
+      if (c >= count) break;
+      out[c * g.out_row] = (T)(v[c] * kPlaneUnscale);
+    }
+  } else {
+    using T = typename std::conditional<kEpilogue == kStepF32, float, __nv_bfloat16>::type;
+    const PullParams& s = p.step;
+    const int matrix = g.first_matrix + t.q / s.workers, worker = t.q % s.workers;
+    const int64_t at = (int64_t)p.matrix_offset[matrix] + (int64_t)n0 * g.out_row + m;
+    const float scale = p.matrix_scale[matrix] * kPlaneUnscale;
+    const int peer = s.peers[worker * s.draw_stride];
+    const bool pull = peer != worker && (uint32_t)peer < (uint32_t)s.workers;
+    const float w = pull ? s.weights[worker * s.draw_stride] : 0.0f;
+    const T* own = (const T*)s.x + worker * s.x_row + at;
+    const T* other = (const T*)s.x + (pull ? peer : worker) * s.x_row + at;
+    T* next = (T*)s.x_next + worker * s.next_row + at;
+#pragma unroll
+    for (int c0 = 0; c0 < 32; c0 += 8) {
+      if (c0 >= count) break;
+      float xi[8], xm[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        xi[c] = c0 + c < count ? (float)own[(c0 + c) * g.out_row] : 0.0f;
+        xm[c] = c0 + c < count ? (float)other[(c0 + c) * g.out_row] : 0.0f;
+      }
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        if (c0 + c >= count) break;
+        const float h = fmaf(-s.lr, fmaf(s.decay, xi[c], scale * v[c0 + c]), xi[c]);
+        next[(c0 + c) * g.out_row] = (T)(pull ? fmaf(-w, h - xm[c], h) : h);
+      }
+    }
+  }
+}
+
+// kPlanes = 2 (fp32 operands): every kPromote steps of 64 k the accumulator goes to fp32 registers and starts over.  The tensor cores drop
+// what lies below the running sum's last bit at every 16 k, so the error grows with k (2-norm, K = 2048: 7.4e-6; with the sum taken over
+// every 128 k 1e-6 at any K); the epilogue warps add a part under the products of the next.
+constexpr int kPromote = 2;
+
+template <int kCtas, int kEpilogue, int kPlanes>
+__global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __grid_constant__ ProductParams p) {
+  extern __shared__ unsigned char raw[];
+  __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 4];
+  __shared__ uint32_t tmem_at;
+  __shared__ volatile uint32_t gave_up;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t rank = kCtas == 2 ? ptx::cluster_rank() : 0;
+  // (the same offset in both CTAs of a pair: dynamic shared memory starts at the same address in every CTA)
+  const uint32_t base = (ptx::smem(raw) + 1023) & ~1023u;
+  const uint32_t full = ptx::smem(bars), empty = full + 8 * kMaxStages, done = empty + 8 * kMaxStages, drained = done + 16;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      ptx::barrier_init(full + 8 * s, 1);
+      ptx::barrier_init(empty + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      ptx::barrier_init(done + 8 * b, 1);
+      ptx::barrier_init(drained + 8 * b, 8 * kCtas);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    gave_up = 0;
+  }
+  if (warp == 9) ptx::tmem_alloc<kCtas>(ptx::smem(&tmem_at), 512);
+  ptx::fence_before();
+  __syncthreads();
+  if (kCtas == 2) ptx::cluster_sync();
+  ptx::fence_after();
+  const uint32_t tmem = tmem_at;
+  ptx::let_successor_start();
+  ptx::wait_for_predecessor();
+  if (p.clear_error && blockIdx.x == 0 && threadIdx.x == 0) *p.error = 0;
+
+  const int first = blockIdx.x / kCtas, stride = gridDim.x / kCtas;
+  auto failed = [&] {
+    gave_up = 1;
+    *(volatile unsigned int*)p.error = 1;
+    __threadfence_system();
+  };
+  if (warp == 8 && ptx::elect()) {  // ---- loads
+    int issued = 0;  // stages filled so far
+    bool ok = true;
+    for (int t = first; t < p.tiles && ok; t += stride) {
+      const Tile tile = find_tile(p, t);
+      const ProductGroup& g = p.group[tile.g];
+      const int rows_b = g.bn / kCtas;
+      const int m0 = (tile.i * kCtas + (int)rank) * 128, n0 = tile.j * g.bn + (int)rank * rows_b;
+      const int qa = g.a_batched ? tile.q : 0, qb = g.b_batched ? tile.q : 0;
+      const int boxes_b = rows_b / kProductBox;
+      const uint32_t bytes = (uint32_t)(kPlanes * (2 + boxes_b) * kBoxBytes) * kCtas;
+      const int steps = (g.K + 63) / 64;
+      for (int kb = 0; kb < steps; ++kb, ++issued) {
+        const int s = issued % p.stages, lap = issued / p.stages;
+        if (lap > 0 && !ptx::wait(empty + 8 * s, (lap - 1) & 1)) { ok = false; break; }
+        if (gave_up) { ok = false; break; }
+        if (rank == 0) ptx::expect_tx(full + 8 * s, bytes);
+        const uint32_t bar = kCtas == 2 ? ptx::map_to(full + 8 * s, 0) : full + 8 * s;
+        const uint32_t at = base + s * p.stage_bytes;
+        for (int plane = 0; plane < kPlanes; ++plane) {
+          for (int b = 0; b < 2; ++b)
+            ptx::load_box<kCtas>(at + plane * p.a_bytes + b * kBoxBytes, &g.a, bar, g.a_mn ? m0 + 64 * b : kb * 64, g.a_mn ? kb * 64 : m0 + 64 * b, qa, plane);
+          for (int b = 0; b < boxes_b; ++b)
+            ptx::load_box<kCtas>(at + kPlanes * p.a_bytes + plane * p.b_bytes + b * kBoxBytes, &g.b, bar, g.b_mn ? n0 + 64 * b : kb * 64,
+                                 g.b_mn ? kb * 64 : n0 + 64 * b, qb, plane);
+        }
+      }
+    }
+    if (!ok) failed();
+    // no CTA leaves while its own copies are under way: what is still in flight ends within the limit of these waits
+    for (int back = min(issued, p.stages); back > 0; --back) {
+      const int k = issued - back, s = k % p.stages, lap = k / p.stages;
+      if (!ptx::wait((ok ? empty : full) + 8 * s, lap & 1) && ok) {
+        ok = false;
+        failed();
+      }
+    }
+  } else if (warp == 9 && rank == 0 && ptx::elect()) {  // ---- products
+    int used = 0, part = 0;  // stages and accumulators so far
+    bool ok = true;
+    for (int t = first; t < p.tiles && ok; t += stride) {
+      const Tile tile = find_tile(p, t);
+      const ProductGroup& g = p.group[tile.g];
+      const uint32_t step_a = g.a_mn ? 2048 : 32, step_b = g.b_mn ? 2048 : 32;  // 16 k further
+      const int steps = (g.K + 63) / 64, per_part = kPlanes == 2 ? kPromote : steps;
+      for (int begin = 0; begin < steps && ok; begin += per_part, ++part) {
+        const int acc = part & 1, lap = part >> 1;
+        if (lap > 0 && !ptx::wait(drained + 8 * acc, (lap - 1) & 1)) { ok = false; break; }
+        ptx::fence_after();
+        const uint32_t d = tmem + acc * 256;
+        for (int kb = begin; kb < min(steps, begin + per_part); ++kb, ++used) {
+          const int s = used % p.stages;
+          if (!ptx::wait(full + 8 * s, (used / p.stages) & 1) || gave_up) { ok = false; break; }
+          ptx::fence_after();
+          const uint32_t at = base + s * p.stage_bytes;
+#pragma unroll
+          for (int term = 0; term < (kPlanes == 2 ? 3 : 1); ++term) {  // hi lo, lo hi, hi hi: the small ones first
+            const uint32_t a = at + (kPlanes == 2 && term == 1 ? p.a_bytes : 0), b = at + kPlanes * p.a_bytes + (kPlanes == 2 && term == 0 ? p.b_bytes : 0);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              ptx::mma<kCtas>(d, ptx::descriptor(a + k * step_a, g.a_mn), ptx::descriptor(b + k * step_b, g.b_mn), g.idesc, kb > begin || term + k > 0);
+          }
+          ptx::commit<kCtas>(empty + 8 * s);
+        }
+        if (ok) ptx::commit<kCtas>(done + 8 * acc);
+      }
+    }
+    if (!ok) failed();
+  } else if (warp < 8) {  // ---- epilogue: warp w has lanes 32 (w % 4) ... of the accumulator and every other 32 columns
+    const uint32_t quadrant = warp % 4, half = warp / 4;
+    int part = 0;
+    bool ok = true;
+    for (int t = first; t < p.tiles && ok; t += stride) {
+      const Tile tile = find_tile(p, t);
+      const ProductGroup& g = p.group[tile.g];
+      const int m = (tile.i * kCtas + (int)rank) * 128 + (int)quadrant * 32 + lane;
+      const int columns = min(g.bn, g.N - tile.j * g.bn);
+      int exponent = 0;
+      if (kEpilogue == kLayerF32) exponent = -(g.exp_a[g.a_batched ? tile.q : 0] + g.exp_b[g.b_batched ? tile.q : 0]);
+      const int steps = (g.K + 63) / 64, per_part = kPlanes == 2 ? kPromote : steps;
+      float sum[kPlanes == 2 ? 4 : 1][32];
+      if (kPlanes == 2) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int c = 0; c < 32; ++c) sum[k][c] = 0.0f;
+      }
+      for (int begin = 0; begin < steps; begin += per_part, ++part) {
+        const int acc = part & 1, lap = part >> 1;
+        if (!__all_sync(0xFFFFFFFFu, ptx::wait(done + 8 * acc, lap & 1))) {
+          if (lane == 0) failed();
+          ok = false;
+          break;
+        }
+        ptx::fence_after();
+        const uint32_t from = tmem + (quadrant * 32 << 16) + acc * 256;
+        if (kPlanes == 2) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int c = (int)half * 32 + 64 * k;
+            if (c < columns) {
+              float v[32];
+              ptx::tmem_load32(from + c, v);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) sum[k][e] += v[e];
+            }
+          }
+        } else {
+          for (int c = (int)half * 32; c < columns; c += 64) {
+            ptx::tmem_load32(from + c, sum[0]);
+            epilogue_chunk<kEpilogue>(p, g, tile, m, tile.j * g.bn + c, exponent, sum[0]);
+          }
+        }
+        ptx::fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (kCtas == 2) ptx::arrive_cluster(ptx::map_to(drained + 8 * acc, 0));
+          else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(drained + 8 * acc) : "memory");
+        }
+      }
+      if (kPlanes == 2 && ok) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int c = (int)half * 32 + 64 * k;
+          if (c < columns) epilogue_chunk<kEpilogue>(p, g, tile, m, tile.j * g.bn + c, exponent, sum[k]);
+        }
+      }
+    }
+  }
+  __syncwarp();
+  ptx::fence_before();
+  __syncthreads();
+  if (kCtas == 2) ptx::cluster_sync();  // (neither CTA's shared memory goes while the other may still signal it)
+  ptx::fence_after();
+  if (warp == 9) ptx::tmem_free<kCtas>(tmem, 512);
+}
+
+}  // namespace netmax
