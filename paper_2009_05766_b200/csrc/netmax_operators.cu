@@ -23,6 +23,7 @@ namespace {
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr size_t kHeader = 256;                      // of a workspace: the error word
 constexpr size_t kProductSmem = (size_t)225 * 1024;  // dynamic shared memory that a launch may take
+constexpr size_t kSlots = 8 * kSlotBytes;            // of it, the epilogue's
 constexpr size_t kLeastSmem = (size_t)120 * 1024;    // more than half an SM's: no two of these CTAs, which take all of TMEM, share one
 
 int fail_op(int code, const char* fmt, ...) {
@@ -192,6 +193,22 @@ ProductKernel pick_product(int epilogue, int planes) {
   }
 }
 
+// The kernels for two planes share their registers out anew (216 a thread for the epilogue, 72 for the others), which waits for good
+// where a launch did not get that many: a build that gave such a kernel fewer than 168 is refused.
+int check_registers(const void* kernel) {
+  static std::mutex mu;
+  static auto* known = new std::unordered_map<const void*, int>();
+  std::lock_guard<std::mutex> lock(mu);
+  int& registers = (*known)[kernel];
+  if (registers == 0) {
+    cudaFuncAttributes a;
+    OP_CUDA(cudaFuncGetAttributes(&a, kernel));
+    registers = a.numRegs;
+  }
+  if (registers * kProductThreads < (2 * 216 + 72) * 128) return fail_op(NETMAX_CUDA_ERROR, "a product kernel was built with %d registers, 168 needed", registers);
+  return NETMAX_OK;
+}
+
 // Chooses the tile shape for all groups of a launch and runs it.
 int run_products(Stream& s, ProductParams& p, const int* batches, bool bf16, int epilogue) {
   const int sms = sm_count();
@@ -226,12 +243,13 @@ int run_products(Stream& s, ProductParams& p, const int* batches, bool bf16, int
   p.a_bytes = 128 * 128;
   p.b_bytes = (uint32_t)most_b * 128;
   p.stage_bytes = (uint32_t)p.planes * (p.a_bytes + p.b_bytes);
-  p.stages = (int)std::min<size_t>(kMaxStages, (kProductSmem - 1024) / p.stage_bytes);
-  const size_t smem = std::max(kLeastSmem, (size_t)1024 + (size_t)p.stages * p.stage_bytes);
+  p.stages = (int)std::min<size_t>(kMaxStages, (kProductSmem - 1024 - kSlots) / p.stage_bytes);
+  const size_t smem = std::max(kLeastSmem, (size_t)1024 + kSlots + (size_t)p.stages * p.stage_bytes);
   p.error = s.error;
   p.clear_error = s.clear;
   ProductKernel kernel = ctas == 2 ? pick_product<2>(epilogue, p.planes) : pick_product<1>(epilogue, p.planes);
   OP_CUDA(raise_smem_limit((const void*)kernel, smem));
+  if (p.planes == 2) OP_DO(check_registers((const void*)kernel));
   const int grid = (int)std::min<int64_t>(tiles, sms / ctas) * ctas;
   OP_DO(launch(s, kernel, dim3(grid), kProductThreads, smem, ctas, p));
   s.clear = false;
@@ -352,7 +370,7 @@ int run_jobs(Stream& s, OperandParams& jobs, int n_jobs, int storage) {
   return launch(s, kernel, dim3(x, y, (unsigned)n_jobs), kElementThreads, 0, 1, jobs);
 }
 
-// One product of a launch: D[m][n] over k, stored at out (m contiguous).
+// One product of a launch: D[m][n] over k.
 void fill_product(ProductGroup& g, const Prepared& a, bool a_mn, const Prepared& b, bool b_mn, int64_t M, int64_t N, int64_t K) {
   g.M = (int32_t)M;
   g.N = (int32_t)N;
@@ -494,9 +512,9 @@ int netmax_layer_forward(const netmax_layer* l) try {
   p.groups = 1;
   p.planes = l->storage == NETMAX_STORAGE_F32 ? 2 : 1;
   ProductGroup& g = p.group[0];
-  fill_product(g, w, false, x, false, n_out, n, n_in);
-  OP_DO(encode(w.operand, &g.a));
-  OP_DO(encode(x.operand, &g.b));
+  fill_product(g, x, false, w, false, n, n_out, n_in);
+  OP_DO(encode(x.operand, &g.a));
+  OP_DO(encode(w.operand, &g.b));
   g.out = l->y.data;
   g.out_row = l->y.row_stride;
   g.out_batch = l->y.worker_stride;
@@ -605,9 +623,9 @@ int netmax_layer_backward(const netmax_layer* l) try {
   if (l->dx.data) {
     ProductGroup& g = p.group[p.groups];
     batches[p.groups++] = l->M;
-    fill_product(g, w, true, dz, false, n_in, n, n_out);
-    OP_DO(encode(w.operand, &g.a));
-    OP_DO(encode(dz.operand, &g.b));
+    fill_product(g, dz, false, w, true, n, n_in, n_out);
+    OP_DO(encode(dz.operand, &g.a));
+    OP_DO(encode(w.operand, &g.b));
     g.out = l->dx.data;
     g.out_row = l->dx.row_stride;
     g.out_batch = l->dx.worker_stride;
@@ -615,9 +633,9 @@ int netmax_layer_backward(const netmax_layer* l) try {
   if (l->dweight.data) {
     ProductGroup& g = p.group[p.groups];
     batches[p.groups++] = l->M;
-    fill_product(g, x, true, dz, true, n_in, n_out, n);
-    OP_DO(encode(x.operand, &g.a));
-    OP_DO(encode(dz.operand, &g.b));
+    fill_product(g, dz, true, x, true, n_out, n_in, n);
+    OP_DO(encode(dz.operand, &g.a));
+    OP_DO(encode(x.operand, &g.b));
     g.out = l->dweight.data;
     g.out_row = l->dweight.row_stride;
     g.out_batch = l->dweight.worker_stride;
@@ -721,12 +739,12 @@ int run_schulz(Stream& s, std::vector<SchulzGroup>& groups, int steps, int plane
               g.residual_plane = q.s_plane;
             }
           } else {
-            g.M = (int32_t)q.cols;
-            g.N = (int32_t)q.rows;
+            g.M = (int32_t)q.rows;
+            g.N = (int32_t)q.cols;
             g.K = (int32_t)q.side;
-            g.a = q.tall ? q.map_poly : q.map_x[now];
-            g.b = q.tall ? q.map_x[now] : q.map_poly;
-            g.a_mn = !q.tall;
+            g.a = q.tall ? q.map_x[now] : q.map_poly;
+            g.b = q.tall ? q.map_poly : q.map_x[now];
+            g.b_mn = !q.tall;
             g.residual = q.x[now];
             g.residual_row = q.x_row;
             g.residual_batch = q.x_batch;

@@ -1,7 +1,7 @@
 // Batched matrix products on the tensor cores (tcgen05, accumulators in TMEM, operands by TMA), one kernel for all of the
 // operators that train real weights in the replicas.
 //
-//   D[m][n] = sum_k A[m][k] B[n][k]        m = the output's contiguous dimension, n = its rows
+//   D[m][n] = sum_k A[m][k] B[n][k]        m = the output's rows, n = its contiguous columns
 //
 // Both operands are 16-bit (fp16 or bf16) and lie in memory either with k contiguous or with m (n) contiguous; the descriptors of the
 // tensor cores and the order of the TMA coordinates say which, so no operand is ever transposed.  fp32 operands come as two
@@ -14,6 +14,12 @@
 // itself.  Problems that would leave SMs without a tile that way take one CTA per tile of 128 x 64 to 128 x 256.  Warps 0-7 are the
 // epilogue, warp 8 issues the TMA loads, warp 9 the products; the accumulators are double-buffered so that the epilogue of a tile
 // runs under the products of the next.
+//
+// A thread of the epilogue reads one row of 32 columns from TMEM.  Handled as they come, loads and stores of such rows touch 32 lines each
+// (and with the roles of rows and columns exchanged 64 bytes each, 22 instructions per 32 elements: the iterates of 8 matrices of 512 x 4608
+// took 104 us a product).  So a warp turns its 32 x 32 values around in 4 KB of shared memory: afterwards a lane has eight columns of every
+// eighth row, everything in global memory moves in 16-byte pieces of whole 64- or 128-byte lines, and the arithmetic has independent
+// elements to interleave.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -25,7 +31,8 @@
 
 namespace netmax {
 
-constexpr int kProductThreads = 320;      // eight epilogue warps, one that loads, one that multiplies
+constexpr int kProductThreads = 384;      // eight epilogue warps, one that loads, one that multiplies, two that fill their warpgroup
+constexpr int kSlotBytes = 4096;          // of an epilogue warp: 32 x 32 fp32
 constexpr int kProductBox = 64;           // a TMA box: 64 rows of 64 16-bit values (128 bytes, the swizzle's width)
 constexpr int kBoxBytes = kProductBox * 128;
 constexpr int kMaxGroups = 12;            // groups of equal matrices in one launch
@@ -53,7 +60,7 @@ struct ProductGroup {
   int32_t bn = 0;              // columns of a tile
   int32_t a_batched = 1, b_batched = 1;  // 0: one matrix for all
   uint32_t idesc = 0;
-  // epilogue: element (n, m) of matrix q at base + q * batch + n * row + m
+  // epilogue: element (m, n) of matrix q at base + q * batch + m * row + n
   void* out = nullptr;
   int64_t out_row = 0, out_batch = 0, out_plane = 0;
   void* z = nullptr;
@@ -221,20 +228,12 @@ __device__ __forceinline__ float activation_slope(float z, int activation) {
   const float s = 1.0f / (1.0f + expf(-z));
   return s * (1.0f + z * (1.0f - s));
 }
-// v 2^e in two factors, so that neither overflows or loses bits where the result does not.
-__device__ __forceinline__ float scale_by_power(float v, int e) {
-  const int half = e / 2;
-  return ldexpf(1.0f, half) * v * ldexpf(1.0f, e - half);
-}
 // The two fp16 planes of a scaled value; what is not finite stays so, once.
 __device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
   hi = __float2half_rn(v);
   const float h = __half2float(hi);
   lo = fabsf(h) <= 65504.0f ? __float2half_rn(v - h) : __float2half_rn(0.0f);
 }
-
-__device__ __forceinline__ uint32_t pack2(__half a, __half b) { return (uint32_t)__half_as_ushort(a) | (uint32_t)__half_as_ushort(b) << 16; }
-__device__ __forceinline__ uint4 pack8(const __half* h) { return make_uint4(pack2(h[0], h[1]), pack2(h[2], h[3]), pack2(h[4], h[5]), pack2(h[6], h[7])); }
 
 struct Tile {
   int g, q, i, j;  // group, matrix, tile row (m) and column (n)
@@ -264,138 +263,213 @@ __device__ __forceinline__ Tile find_tile(const ProductParams& p, int t) {
   return r;
 }
 
-// 32 columns of one row m of the accumulator: element (n0 + c, m) for c = 0 ... 31.
-template <int kEpilogue>
-__device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const ProductGroup& g, const Tile& t, int m, int n0, int exponent, float (&v)[32]) {
-  if (m >= g.M) return;
-  const int count = min(32, g.N - n0);  // (the same for the whole warp)
+// Eight values of a type, in 16-byte pieces where the address allows it; `count` of them exist.
+template <typename T>
+__device__ __forceinline__ void load8(const T* at, int count, float (&v)[8]) {
+  if (count == 8 && ((uintptr_t)at & 15) == 0) {
+    if (sizeof(T) == 4) {
+      const float4 a = ((const float4*)at)[0], b = ((const float4*)at)[1];
+      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    } else {
+      const uint4 a = *(const uint4*)at;
+      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[2 * k] = __uint_as_float(w[k] << 16);
+        v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = k < count ? (float)at[k] : 0.0f;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *(const uint32_t*)&h;
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* at, int count, const float (&v)[8]) {
+  if (count == 8 && ((uintptr_t)at & 15) == 0) {
+    if (sizeof(T) == 4) {
+      ((float4*)at)[0] = make_float4(v[0], v[1], v[2], v[3]);
+      ((float4*)at)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+      *(uint4*)at = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (k < count) at[k] = (T)v[k];
+}
+__device__ __forceinline__ void unpack_half(const uint4& a, float (&v)[8]) {
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 f = __half22float2(*(const __half2*)&w[k]);
+    v[2 * k] = f.x;
+    v[2 * k + 1] = f.y;
+  }
+}
+// Eight values as two planes.
+__device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const __half2 a = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+    const float2 f = __half22float2(a);
+    const __half2 b = __floats2half2_rn(fabsf(f.x) <= 65504.0f ? v[2 * k] - f.x : 0.0f, fabsf(f.y) <= 65504.0f ? v[2 * k + 1] - f.y : 0.0f);
+    h[k] = *(const uint32_t*)&a;
+    l[k] = *(const uint32_t*)&b;
+  }
+  hi = make_uint4(h[0], h[1], h[2], h[3]);
+  lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+// What an epilogue reads besides the accumulator: rows i * 8 + lane / 4, columns 8 (lane % 4) ... of a chunk, both planes.
+struct Residual {
+  uint4 hi[4], lo[4];
+};
+template <int kEpilogue, int kPlanes>
+__device__ __forceinline__ void load_residual(const ProductGroup& g, int q, int m0, int n0, int lane, Residual& r) {
+  if (kEpilogue < kPolynomial) return;
+  const int n = n0 + 8 * (lane % 4);
+  const __half* at = (const __half*)g.residual + q * g.residual_batch + n;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int m = m0 + 8 * i + lane / 4;
+    r.hi[i] = r.lo[i] = make_uint4(0, 0, 0, 0);
+    if (m < g.M && n < g.N) {  // (planes' rows are padded to eight columns)
+      r.hi[i] = *(const uint4*)(at + (int64_t)m * g.residual_row);
+      if (kEpilogue > kPolynomial || kPlanes == 2) r.lo[i] = *(const uint4*)(at + (int64_t)m * g.residual_row + g.residual_plane);
+    }
+  }
+}
+
+// Rows m0 ... m0 + 31 and columns n0 ... n0 + 31 of the accumulator: v is row m0 + lane.  `slot`: the warp's 4 KB.
+template <int kEpilogue, int kPlanes>
+__device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const ProductGroup& g, const Tile& t, int m0, int n0, int exponent, const float (&acc)[32],
+                                               float* slot, const Residual& residual) {
+  const int lane = threadIdx.x % 32;
+  __syncwarp();
+#pragma unroll
+  for (int c = 0; c < 8; ++c)  // 16-byte pieces, the row's number folded in: neither direction meets a bank twice
+    *(float4*)(slot + lane * 32 + (c ^ (lane & 7)) * 4) = make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
+  __syncwarp();
+  const int c = lane % 4, n = n0 + 8 * c, count = min(8, g.N - n);
+  const bool mirrored = (kEpilogue == kGram || kEpilogue == kPolynomial) && t.i != t.j;
+  float bias[8];
   if (kEpilogue == kLayerF32 || kEpilogue == kLayerBf16) {
     using T = typename std::conditional<kEpilogue == kLayerF32, float, __nv_bfloat16>::type;
-    const float bias = g.bias ? (float)((const T*)g.bias)[t.q * g.bias_batch + m] : 0.0f;
-    const T* r = g.residual ? (const T*)g.residual + t.q * g.residual_batch + n0 * g.residual_row + m : nullptr;
-    T* z = g.z ? (T*)g.z + t.q * g.z_batch + n0 * g.z_row + m : nullptr;
-    T* y = (T*)g.out + t.q * g.out_batch + n0 * g.out_row + m;
+    const T* b = g.bias && count > 0 ? (const T*)g.bias + t.q * g.bias_batch + n : nullptr;
 #pragma unroll
-    for (int c0 = 0; c0 < 32; c0 += 8) {
-      if (c0 >= count) break;
+    for (int k = 0; k < 8; ++k) bias[k] = b && k < count ? (float)b[k] : 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = 8 * i + lane / 4, m = m0 + row;
+    float4* at0 = (float4*)(slot + row * 32 + ((2 * c) ^ (row & 7)) * 4);
+    float4* at1 = (float4*)(slot + row * 32 + ((2 * c + 1) ^ (row & 7)) * 4);
+    const float4 a0 = *at0, a1 = *at1;
+    float v[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
+    if (m >= g.M || count <= 0) continue;
+    if (kEpilogue == kLayerF32 || kEpilogue == kLayerBf16) {
+      using T = typename std::conditional<kEpilogue == kLayerF32, float, __nv_bfloat16>::type;
+      if (kEpilogue == kLayerF32) {
+        const float f0 = ldexpf(1.0f, exponent / 2), f1 = ldexpf(1.0f, exponent - exponent / 2);  // (in two factors: neither overflows)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = v[k] * f0 * f1;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += bias[k];
       float add[8];
+      if (g.residual) load8((const T*)g.residual + t.q * g.residual_batch + m * g.residual_row + n, count, add);
+      if (g.z) store8((T*)g.z + t.q * g.z_batch + m * g.z_row + n, count, v);
+      if (g.activation == kActRelu) {
 #pragma unroll
-      for (int c = 0; c < 8; ++c) add[c] = r && c0 + c < count ? (float)r[(c0 + c) * g.residual_row] : 0.0f;
+        for (int k = 0; k < 8; ++k) v[k] = activate(v[k], kActRelu);
+      } else if (g.activation == kActGelu) {
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        if (c0 + c >= count) break;
-        float s = v[c0 + c];
-        if (kEpilogue == kLayerF32) s = scale_by_power(s, exponent);
-        s += bias;
-        if (z) z[(c0 + c) * g.z_row] = (T)s;
-        s = activate(s, g.activation);
-        if (r) s += add[c];
-        y[(c0 + c) * g.out_row] = (T)s;
+        for (int k = 0; k < 8; ++k) v[k] = activate(v[k], kActGelu);
+      } else if (g.activation == kActSilu) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = activate(v[k], kActSilu);
+      }
+      if (g.residual) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += add[k];
+      }
+      store8((T*)g.out + t.q * g.out_batch + m * g.out_row + n, count, v);
+      continue;
+    }
+    float hi[8], lo[8];
+    if (kEpilogue >= kPolynomial) {
+      unpack_half(residual.hi[i], hi);
+      if (kEpilogue > kPolynomial || kPlanes == 2) {
+        unpack_half(residual.lo[i], lo);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) hi[k] += lo[k];
       }
     }
-    return;
-  }
-  if (kEpilogue == kGram || kEpilogue == kPolynomial) {
-    const bool two = p.planes == 2;
-    const int64_t at = t.q * g.out_batch + (int64_t)n0 * g.out_row + m;
-    __half before[2][32];
-    if (kEpilogue == kPolynomial) {
-      const __half* a = (const __half*)g.residual + t.q * g.residual_batch + (int64_t)n0 * g.residual_row + m;
 #pragma unroll
-      for (int c = 0; c < 32; ++c) {
-        before[0][c] = c < count ? a[c * g.residual_row] : __half(0.0f);
-        before[1][c] = two && c < count ? a[c * g.residual_row + g.residual_plane] : __half(0.0f);
+    for (int k = 0; k < 8; ++k) {
+      v[k] *= kPlaneUnscale;
+      if (kEpilogue == kPolynomial) v[k] = fmaf(p.cc, v[k], p.cb * hi[k]);
+      if (kEpilogue > kPolynomial) v[k] = fmaf(p.ca, hi[k], v[k]);
+    }
+    if (kEpilogue == kGram || kEpilogue == kPolynomial || kEpilogue == kUpdate) {
+      uint4 h, l;
+      split8(v, h, l);
+      __half* out = (__half*)g.out + t.q * g.out_batch + m * g.out_row + n;
+      *(uint4*)out = h;
+      if (kEpilogue == kUpdate || kPlanes == 2) *(uint4*)(out + g.out_plane) = l;
+      if (mirrored) {  // both planes of an element in one word
+        *at0 = make_float4(__uint_as_float(__byte_perm(h.x, l.x, 0x5410)), __uint_as_float(__byte_perm(h.x, l.x, 0x7632)),
+                           __uint_as_float(__byte_perm(h.y, l.y, 0x5410)), __uint_as_float(__byte_perm(h.y, l.y, 0x7632)));
+        *at1 = make_float4(__uint_as_float(__byte_perm(h.z, l.z, 0x5410)), __uint_as_float(__byte_perm(h.z, l.z, 0x7632)),
+                           __uint_as_float(__byte_perm(h.w, l.w, 0x5410)), __uint_as_float(__byte_perm(h.w, l.w, 0x7632)));
       }
+      continue;
     }
-    __half* out = (__half*)g.out;
-    __half hi[32], lo[32];
+    if (kEpilogue == kLastF32 || kEpilogue == kLastBf16) {
+      using T = typename std::conditional<kEpilogue == kLastF32, float, __nv_bfloat16>::type;
 #pragma unroll
-    for (int c = 0; c < 32; ++c) {
-      float s = v[c] * kPlaneUnscale;
-      if (kEpilogue == kPolynomial) s = p.cb * (__half2float(before[0][c]) + __half2float(before[1][c])) + p.cc * s;
-      split(s, hi[c], lo[c]);
+      for (int k = 0; k < 8; ++k) v[k] *= kPlaneUnscale;
+      store8((T*)g.out + t.q * g.out_batch + m * g.out_row + n, count, v);
+      continue;
     }
-#pragma unroll
-    for (int c = 0; c < 32; ++c) {
-      if (c >= count) break;
-      out[at + c * g.out_row] = hi[c];
-      if (two) out[at + c * g.out_row + g.out_plane] = lo[c];
-    }
-    if (t.i != t.j) {  // the mirrored half: this thread's columns are contiguous there
-      __half* mirror = out + t.q * g.out_batch + (int64_t)m * g.out_row + n0;
-      if (count == 32) {
-#pragma unroll
-        for (int c = 0; c < 32; c += 8) *(uint4*)(mirror + c) = pack8(hi + c);
-        if (two) {
-#pragma unroll
-          for (int c = 0; c < 32; c += 8) *(uint4*)(mirror + g.out_plane + c) = pack8(lo + c);
-        }
-      } else {
-#pragma unroll
-        for (int c = 0; c < 32; ++c) {
-          if (c >= count) break;
-          mirror[c] = hi[c];
-          if (two) mirror[g.out_plane + c] = lo[c];
-        }
-      }
-    }
-    return;
-  }
-  // a X + D: X always comes in two planes (fp32's accuracy), whatever the products take
-  __half x[2][32];
-  const __half* a = (const __half*)g.residual + t.q * g.residual_batch + (int64_t)n0 * g.residual_row + m;
-#pragma unroll
-  for (int c = 0; c < 32; ++c) {
-    x[0][c] = c < count ? a[c * g.residual_row] : __half(0.0f);
-    x[1][c] = c < count ? a[c * g.residual_row + g.residual_plane] : __half(0.0f);
-  }
-#pragma unroll
-  for (int c = 0; c < 32; ++c) v[c] = p.ca * (__half2float(x[0][c]) + __half2float(x[1][c])) + v[c] * kPlaneUnscale;
-  if (kEpilogue == kUpdate) {
-    __half* out = (__half*)g.out + t.q * g.out_batch + (int64_t)n0 * g.out_row + m;
-#pragma unroll
-    for (int c = 0; c < 32; ++c) {
-      if (c >= count) break;
-      __half hi, lo;
-      split(v[c], hi, lo);
-      out[c * g.out_row] = hi;
-      out[c * g.out_row + g.out_plane] = lo;
-    }
-  } else if (kEpilogue == kLastF32 || kEpilogue == kLastBf16) {
-    using T = typename std::conditional<kEpilogue == kLastF32, float, __nv_bfloat16>::type;
-    T* out = (T*)g.out + t.q * g.out_batch + (int64_t)n0 * g.out_row + m;
-#pragma unroll
-    for (int c = 0; c < 32; ++c) {
-      if (c >= count) break;
-      out[c * g.out_row] = (T)(v[c] * kPlaneUnscale);
-    }
-  } else {
     using T = typename std::conditional<kEpilogue == kStepF32, float, __nv_bfloat16>::type;
     const PullParams& s = p.step;
     const int matrix = g.first_matrix + t.q / s.workers, worker = t.q % s.workers;
-    const int64_t at = (int64_t)p.matrix_offset[matrix] + (int64_t)n0 * g.out_row + m;
+    const int64_t at = (int64_t)p.matrix_offset[matrix] + m * g.out_row + n;
     const float scale = p.matrix_scale[matrix] * kPlaneUnscale;
     const int peer = s.peers[worker * s.draw_stride];
     const bool pull = peer != worker && (uint32_t)peer < (uint32_t)s.workers;
     const float w = pull ? s.weights[worker * s.draw_stride] : 0.0f;
-    const T* own = (const T*)s.x + worker * s.x_row + at;
-    const T* other = (const T*)s.x + (pull ? peer : worker) * s.x_row + at;
-    T* next = (T*)s.x_next + worker * s.next_row + at;
+    float xi[8], xm[8];
+    load8((const T*)s.x + worker * s.x_row + at, count, xi);
+    load8((const T*)s.x + (pull ? peer : worker) * s.x_row + at, count, xm);
 #pragma unroll
-    for (int c0 = 0; c0 < 32; c0 += 8) {
-      if (c0 >= count) break;
-      float xi[8], xm[8];
+    for (int k = 0; k < 8; ++k) {
+      const float h = fmaf(-s.lr, fmaf(s.decay, xi[k], scale * v[k]), xi[k]);
+      v[k] = pull ? fmaf(-w, h - xm[k], h) : h;
+    }
+    store8((T*)s.x_next + worker * s.next_row + at, count, v);
+  }
+  if (mirrored) {  // rows n0 + ..., columns m0 + ...
+    __syncwarp();
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        xi[c] = c0 + c < count ? (float)own[(c0 + c) * g.out_row] : 0.0f;
-        xm[c] = c0 + c < count ? (float)other[(c0 + c) * g.out_row] : 0.0f;
-      }
+    for (int i = 0; i < 4; ++i) {
+      const int column = 8 * i + lane / 4, m = m0 + 8 * c;
+      uint32_t w[8];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        if (c0 + c >= count) break;
-        const float h = fmaf(-s.lr, fmaf(s.decay, xi[c], scale * v[c0 + c]), xi[c]);
-        next[(c0 + c) * g.out_row] = (T)(pull ? fmaf(-w, h - xm[c], h) : h);
-      }
+      for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(slot[(8 * c + k) * 32 + ((column / 4) ^ k) * 4 + column % 4]);
+      if (n0 + column >= g.N || m >= g.M) continue;
+      __half* out = (__half*)g.out + t.q * g.out_batch + (int64_t)(n0 + column) * g.out_row + m;
+      *(uint4*)out = make_uint4(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[4], w[5], 0x5410), __byte_perm(w[6], w[7], 0x5410));
+      if (kPlanes == 2)
+        *(uint4*)(out + g.out_plane) = make_uint4(__byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632), __byte_perm(w[4], w[5], 0x7632), __byte_perm(w[6], w[7], 0x7632));
     }
   }
 }
@@ -415,6 +489,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
   const uint32_t rank = kCtas == 2 ? ptx::cluster_rank() : 0;
   // (the same offset in both CTAs of a pair: dynamic shared memory starts at the same address in every CTA)
   const uint32_t base = (ptx::smem(raw) + 1023) & ~1023u;
+  float* const slots = (float*)(raw + (base - ptx::smem(raw)) + (size_t)p.stages * p.stage_bytes);
   const uint32_t full = ptx::smem(bars), empty = full + 8 * kMaxStages, done = empty + 8 * kMaxStages, drained = done + 16;
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
@@ -444,6 +519,9 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
     *(volatile unsigned int*)p.error = 1;
     __threadfence_system();
   };
+  // Two planes: 128 of an epilogue thread's registers are sums.  168 a thread at the launch, 64,512 in all: (2 x 216 + 72) x 128.
+  if (warp >= 8) {
+  if (kPlanes == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   if (warp == 8 && ptx::elect()) {  // ---- loads
     int issued = 0;  // stages filled so far
     bool ok = true;
@@ -512,18 +590,23 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
       }
     }
     if (!ok) failed();
-  } else if (warp < 8) {  // ---- epilogue: warp w has lanes 32 (w % 4) ... of the accumulator and every other 32 columns
+  }
+  } else {  // ---- epilogue: warp w has lanes 32 (w % 4) ... of the accumulator and every other 32 columns
+    if (kPlanes == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const uint32_t quadrant = warp % 4, half = warp / 4;
+    float* const slot = slots + warp * (kSlotBytes / 4);
     int part = 0;
     bool ok = true;
     for (int t = first; t < p.tiles && ok; t += stride) {
       const Tile tile = find_tile(p, t);
       const ProductGroup& g = p.group[tile.g];
-      const int m = (tile.i * kCtas + (int)rank) * 128 + (int)quadrant * 32 + lane;
-      const int columns = min(g.bn, g.N - tile.j * g.bn);
+      const int m0 = (tile.i * kCtas + (int)rank) * 128 + (int)quadrant * 32, n0 = tile.j * g.bn;
+      const int columns = m0 < g.M ? min(g.bn, g.N - n0) : 0;
       int exponent = 0;
       if (kEpilogue == kLayerF32) exponent = -(g.exp_a[g.a_batched ? tile.q : 0] + g.exp_b[g.b_batched ? tile.q : 0]);
       const int steps = (g.K + 63) / 64, per_part = kPlanes == 2 ? kPromote : steps;
+      Residual residual;
+      if (kPlanes == 1 && (int)half * 32 < columns) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + (int)half * 32, lane, residual);
       float sum[kPlanes == 2 ? 4 : 1][32];
       if (kPlanes == 2) {
 #pragma unroll
@@ -552,9 +635,16 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
             }
           }
         } else {
-          for (int c = (int)half * 32; c < columns; c += 64) {
-            ptx::tmem_load32(from + c, sum[0]);
-            epilogue_chunk<kEpilogue>(p, g, tile, m, tile.j * g.bn + c, exponent, sum[0]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int c = (int)half * 32 + 64 * k;
+            if (c < columns) {
+              Residual next;  // of the next 32 columns, under this one's arithmetic
+              if (c + 64 < columns) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + c + 64, lane, next);
+              ptx::tmem_load32(from + c, sum[0]);
+              epilogue_chunk<kEpilogue, kPlanes>(p, g, tile, m0, n0 + c, exponent, sum[0], slot, residual);
+              residual = next;
+            }
           }
         }
         ptx::fence_before();
@@ -568,7 +658,10 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int c = (int)half * 32 + 64 * k;
-          if (c < columns) epilogue_chunk<kEpilogue>(p, g, tile, m, tile.j * g.bn + c, exponent, sum[k]);
+          if (c < columns) {
+            load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + c, lane, residual);
+            epilogue_chunk<kEpilogue, kPlanes>(p, g, tile, m0, n0 + c, exponent, sum[k], slot, residual);
+          }
         }
       }
     }
