@@ -216,16 +216,17 @@ __device__ __forceinline__ uint64_t descriptor(uint32_t at, bool mn) {
 }
 }  // namespace ptx
 
+// Both to a few units of 2^-24 of |z|, which is what a sum's rounding leaves of z.
 __device__ __forceinline__ float activate(float z, int activation) {
   if (activation == kActRelu) return z > 0.0f ? z : (z != z ? z : 0.0f);
-  if (activation == kActGelu) return 0.5f * z * erfcf(z * -0.70710678118654752f);
-  if (activation == kActSilu) return z / (1.0f + expf(-z));
+  if (activation == kActGelu) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+  if (activation == kActSilu) return __fdividef(z, 1.0f + __expf(-z));
   return z;
 }
 __device__ __forceinline__ float activation_slope(float z, int activation) {
   if (activation == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
-  if (activation == kActGelu) return 0.5f * erfcf(z * -0.70710678118654752f) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
-  const float s = 1.0f / (1.0f + expf(-z));
+  if (activation == kActGelu) return fmaf(z * 0.39894228040143268f, __expf(-0.5f * z * z), 0.5f * (1.0f + erff(z * 0.70710678118654752f)));
+  const float s = __fdividef(1.0f, 1.0f + __expf(-z));
   return s * (1.0f + z * (1.0f - s));
 }
 // The two fp16 planes of a scaled value; what is not finite stays so, once.
@@ -347,15 +348,21 @@ __device__ __forceinline__ void load_residual(const ProductGroup& g, int q, int 
   }
 }
 
-// Rows m0 ... m0 + 31 and columns n0 ... n0 + 31 of the accumulator: v is row m0 + lane.  `slot`: the warp's 4 KB.
-template <int kEpilogue, int kPlanes>
-__device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const ProductGroup& g, const Tile& t, int m0, int n0, int exponent, const float (&acc)[32],
-                                               float* slot, const Residual& residual) {
+// A thread's 32 columns into its row of the warp's 4 KB: 16-byte pieces, the row's number folded in, so that neither direction meets a
+// bank twice.
+__device__ __forceinline__ void stage_row(float* slot, const float (&acc)[32]) {
   const int lane = threadIdx.x % 32;
-  __syncwarp();
 #pragma unroll
-  for (int c = 0; c < 8; ++c)  // 16-byte pieces, the row's number folded in: neither direction meets a bank twice
+  for (int c = 0; c < 8; ++c)
     *(float4*)(slot + lane * 32 + (c ^ (lane & 7)) * 4) = make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
+}
+
+// Rows m0 ... m0 + 31 and columns n0 ... n0 + 31 of the accumulator, which the warp has staged.  Called from one place in a loop: unrolled
+// over a tile's chunks the code outgrew the instruction cache (the 8 x (4096 x 4096 x 4096) layer with silu: 1715 us).
+template <int kEpilogue, int kPlanes>
+__device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const ProductGroup& g, const Tile& t, int m0, int n0, int exponent, float* slot,
+                                               const Residual& residual) {
+  const int lane = threadIdx.x % 32;
   __syncwarp();
   const int c = lane % 4, n = n0 + 8 * c, count = min(8, g.N - n);
   const bool mirrored = (kEpilogue == kGram || kEpilogue == kPolynomial) && t.i != t.j;
@@ -635,16 +642,15 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
             }
           }
         } else {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int c = (int)half * 32 + 64 * k;
-            if (c < columns) {
-              Residual next;  // of the next 32 columns, under this one's arithmetic
-              if (c + 64 < columns) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + c + 64, lane, next);
-              ptx::tmem_load32(from + c, sum[0]);
-              epilogue_chunk<kEpilogue, kPlanes>(p, g, tile, m0, n0 + c, exponent, sum[0], slot, residual);
-              residual = next;
-            }
+#pragma unroll 1
+          for (int c = (int)half * 32; c < columns; c += 64) {
+            Residual next;  // of the next 32 columns, under this one's arithmetic
+            if (c + 64 < columns) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + c + 64, lane, next);
+            ptx::tmem_load32(from + c, sum[0]);
+            __syncwarp();
+            stage_row(slot, sum[0]);
+            epilogue_chunk<kEpilogue, kPlanes>(p, g, tile, m0, n0 + c, exponent, slot, residual);
+            residual = next;
           }
         }
         ptx::fence_before();
@@ -655,13 +661,17 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
         }
       }
       if (kPlanes == 2 && ok) {
-#pragma unroll
+#pragma unroll 1
         for (int k = 0; k < 4; ++k) {
           const int c = (int)half * 32 + 64 * k;
-          if (c < columns) {
-            load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + c, lane, residual);
-            epilogue_chunk<kEpilogue, kPlanes>(p, g, tile, m0, n0 + c, exponent, sum[k], slot, residual);
-          }
+          if (c >= columns) break;
+          load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + c, lane, residual);
+          __syncwarp();
+          if (k == 0) stage_row(slot, sum[0]);
+          else if (k == 1) stage_row(slot, sum[kPlanes == 2 ? 1 : 0]);
+          else if (k == 2) stage_row(slot, sum[kPlanes == 2 ? 2 : 0]);
+          else stage_row(slot, sum[kPlanes == 2 ? 3 : 0]);
+          epilogue_chunk<kEpilogue, kPlanes>(p, g, tile, m0, n0 + c, exponent, slot, residual);
         }
       }
     }
