@@ -467,7 +467,8 @@ typedef struct netmax_view {
 
 enum { NETMAX_ACTIVATION_NONE = 0, NETMAX_ACTIVATION_RELU = 1, NETMAX_ACTIVATION_GELU = 2, NETMAX_ACTIVATION_SILU = 3 };
 
-/* A layer of M workers: z = x W^T + bias, y = act(z) + residual, for n rows (n >= 0; n * n_in, n * n_out and n_in * n_out < 2^31).
+/* A layer of M workers: z = x W^T + bias, y = act(z) + residual, for n rows (n >= 0; sizes up to 2^30 with n * n_in, n * n_out and
+ * n_in * n_out < 2^31).
  * gelu is z Phi(z), silu z / (1 + exp(-z)). */
 typedef struct netmax_layer {
   int32_t M;
@@ -503,7 +504,7 @@ int netmax_layer_backward(const netmax_layer* layer);
  */
 typedef struct netmax_orthogonal {
   int32_t count;
-  int64_t rows, cols;    /* rows * cols < 2^31 */
+  int64_t rows, cols;    /* up to 2^30 each, rows * cols < 2^31 */
   int32_t storage;
   int32_t steps;         /* 1 ... 20 */
   netmax_view u;         /* worker_stride: from one matrix to the next */

@@ -267,6 +267,23 @@ struct Prepared {
   int32_t* exponent = nullptr;
 };
 
+Sweep make_sweep(int count, int64_t rows, int64_t cols) {
+  Sweep s;
+  s.rows = (int32_t)rows;
+  s.cols = (int32_t)cols;
+  s.count = count;
+  while (s.shift < 5 && (8 << s.shift) < cols) ++s.shift;
+  s.col_tiles = (int)ceil_div<int64_t>(cols, 8 << s.shift);
+  // up to sixteen rows a thread; fewer where an SM would have less than two CTAs
+  const int lanes = kElementThreads >> s.shift;
+  int each = 16;
+  while (each > 1 && (int64_t)count * s.col_tiles * ceil_div<int64_t>(rows, (int64_t)lanes * each) < 296) each /= 2;
+  s.rows_per_block = lanes * each;
+  s.row_blocks = (int)std::max<int64_t>(1, ceil_div<int64_t>(rows, s.rows_per_block));
+  return s;
+}
+int blocks_of(const Sweep& s) { return s.col_tiles * s.row_blocks; }
+
 // Room for an operand of `count` matrices of rows x cols that has to be laid out.
 struct OperandRoom {
   void* planes = nullptr;
@@ -278,7 +295,8 @@ OperandRoom take_operand(Carver& c, int count, int64_t rows, int64_t cols, int s
   const size_t values = (size_t)count * (size_t)rows * (size_t)up8(cols);
   r.planes = c.take(values * 2 * (storage == NETMAX_STORAGE_F32 ? 2 : 1));
   if (storage == NETMAX_STORAGE_F32) {
-    r.maxima = (float*)c.take((size_t)count * kMaxParts * sizeof(float));
+    // (a shared matrix is swept as one, in up to as many blocks as all of them)
+    r.maxima = (float*)c.take(std::max((size_t)count * blocks_of(make_sweep(count, rows, cols)), (size_t)blocks_of(make_sweep(1, rows, cols))) * sizeof(float));
     r.exponent = (int32_t*)c.take((size_t)count * sizeof(int32_t));
   }
   return r;
@@ -295,9 +313,21 @@ LayerRoom layer_room(void* workspace, int M, int64_t n, int64_t n_in, int64_t n_
   r.x = take_operand(c, M, n, n_in, storage);
   r.weight = take_operand(c, M, n_out, n_in, storage);
   r.dz = take_operand(c, M, n, n_out, storage);
-  r.sums = (float*)c.take((size_t)M * (size_t)ceil_div<int64_t>(n, kSumRows) * (size_t)n_out * sizeof(float));
+  r.sums = (float*)c.take((size_t)M * (size_t)make_sweep(M, n, n_out).row_blocks * (size_t)n_out * sizeof(float));
   r.total = c.used;
   return r;
+}
+
+void fill_source(OperandJob& j, const netmax_view& v, const netmax_view* z, int activation, int count, int64_t rows, int64_t cols) {
+  j.sweep = make_sweep(count, rows, cols);
+  j.src = v.data;
+  j.row = v.row_stride;
+  j.batch = v.worker_stride;
+  if (!z) return;
+  j.z = z->data;
+  j.z_row = z->row_stride;
+  j.z_batch = z->worker_stride;
+  j.activation = activation;
 }
 
 // Either the view itself, where the tensor cores can read it, or a job that lays it out.
@@ -319,19 +349,7 @@ Prepared prepare_operand(const netmax_view& v, const netmax_view* z, int activat
     return r;
   }
   OperandJob& j = jobs.job[n_jobs++];
-  j.src = v.data;
-  j.row = v.row_stride;
-  j.batch = v.worker_stride;
-  if (z) {
-    j.z = z->data;
-    j.z_row = z->row_stride;
-    j.z_batch = z->worker_stride;
-    j.activation = activation;
-  }
-  j.rows = (int32_t)rows;
-  j.cols = (int32_t)cols;
-  j.count = matrices;
-  j.parts = (int)std::min<int64_t>(kMaxParts, ceil_div<int64_t>(rows * cols, kElementThreads * 8));
+  fill_source(j, v, z, activation, matrices, rows, cols);
   j.dst = room.planes;
   j.dst_row = up8(cols);
   j.dst_batch = rows * j.dst_row;
@@ -349,25 +367,24 @@ Prepared prepare_operand(const netmax_view& v, const netmax_view* z, int activat
 
 int run_jobs(Stream& s, OperandParams& jobs, int n_jobs, int storage) {
   if (n_jobs == 0) return NETMAX_OK;
-  int count = 1, parts = 1;
-  int64_t most = 1;
+  int count = 1, blocks = 1;
+  bool laid_out = storage == NETMAX_STORAGE_BF16;
   for (int k = 0; k < n_jobs; ++k) {
-    count = std::max(count, jobs.job[k].count);
-    parts = std::max(parts, jobs.job[k].parts);
-    most = std::max(most, (int64_t)jobs.job[k].rows * jobs.job[k].cols);
+    count = std::max(count, jobs.job[k].sweep.count);
+    blocks = std::max(blocks, blocks_of(jobs.job[k].sweep));
+    laid_out = laid_out || jobs.job[k].dst;
   }
   jobs.error = s.error;
-  const unsigned y = (unsigned)std::min(count, 32768);
+  const dim3 grid((unsigned)blocks, (unsigned)std::min(count, 32768), (unsigned)n_jobs);
   if (storage == NETMAX_STORAGE_F32) {
     jobs.clear_error = s.clear;
-    OP_DO(launch(s, operand_maxima_kernel, dim3((unsigned)parts, y, (unsigned)n_jobs), kElementThreads, 0, 1, jobs));
     s.clear = false;
+    OP_DO(launch(s, operand_maxima_kernel, grid, kElementThreads, 0, 1, jobs));
   }
+  if (!laid_out) return NETMAX_OK;
   jobs.clear_error = s.clear;
   s.clear = false;
-  const unsigned x = (unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div<int64_t>(most, kElementThreads * 4), 1024));
-  auto kernel = storage == NETMAX_STORAGE_F32 ? operand_kernel<float> : operand_kernel<__nv_bfloat16>;
-  return launch(s, kernel, dim3(x, y, (unsigned)n_jobs), kElementThreads, 0, 1, jobs);
+  return launch(s, storage == NETMAX_STORAGE_F32 ? operand_kernel<float> : operand_kernel<__nv_bfloat16>, grid, kElementThreads, 0, 1, jobs);
 }
 
 // One product of a launch: D[m][n] over k.
@@ -423,10 +440,10 @@ int check_workspace(const void* workspace, size_t bytes, size_t needed) {
 }
 int check_layer_sizes(int32_t M, int64_t n, int64_t n_in, int64_t n_out, int32_t storage) {
   OP_DO(check_storage(storage));
-  const int64_t limit = (int64_t)1 << 31;
+  const int64_t limit = (int64_t)1 << 31, most = (int64_t)1 << 30;  // (indices of a row or column, with a tile's overhang, fit 32 bits)
   if (M < 1 || M > 16384) return fail_op(NETMAX_INVALID_ARG, "M = %d outside [1, 16384]", M);
-  if (n < 0 || n_in < 1 || n_out < 1 || n >= limit || n_in >= limit || n_out >= limit || n * n_in >= limit || n * n_out >= limit || n_in * n_out >= limit)
-    return fail_op(NETMAX_INVALID_ARG, "n = %lld, n_in = %lld, n_out = %lld: sizes must be positive (n may be 0) and their products below 2^31", (long long)n,
+  if (n < 0 || n_in < 1 || n_out < 1 || n > most || n_in > most || n_out > most || n * n_in >= limit || n * n_out >= limit || n_in * n_out >= limit)
+    return fail_op(NETMAX_INVALID_ARG, "n = %lld, n_in = %lld, n_out = %lld: sizes must be positive (n may be 0), at most 2^30 each, and their products below 2^31", (long long)n,
                    (long long)n_in, (long long)n_out);
   return NETMAX_OK;
 }
@@ -582,36 +599,24 @@ int netmax_layer_backward(const netmax_layer* l) try {
   Prepared dz, w, x;
   if (l->dx.data || l->dweight.data)
     dz = prepare_operand(l->dy, active ? &l->z : nullptr, l->activation, l->M, n, n_out, l->storage, room.dz, jobs, n_jobs);
+  const bool laid_out = n_jobs > 0 && jobs.job[0].sweep.count == l->M;  // dz, for every worker
   if (l->dx.data) w = prepare_operand(l->weight, nullptr, 0, l->M, n_out, n_in, l->storage, room.weight, jobs, n_jobs);
   if (l->dweight.data) x = prepare_operand(l->x, nullptr, 0, l->M, n, n_in, l->storage, room.x, jobs, n_jobs);
+  if (l->dbias.data) {  // along with dz where that is laid out
+    const int at = laid_out ? 0 : n_jobs++;
+    if (!laid_out) fill_source(jobs.job[at], l->dy, active ? &l->z : nullptr, l->activation, l->M, n, n_out);
+    jobs.job[at].sums = room.sums;
+  }
   OP_DO(run_jobs(s, jobs, n_jobs, l->storage));
   if (l->dbias.data) {
-    OperandJob j;
-    j.src = l->dy.data;
-    j.row = l->dy.row_stride;
-    j.batch = l->dy.worker_stride;
-    if (active) {
-      j.z = l->z.data;
-      j.z_row = l->z.row_stride;
-      j.z_batch = l->z.worker_stride;
-      j.activation = l->activation;
-    }
-    j.rows = (int32_t)n;
-    j.cols = (int32_t)n_out;
-    j.count = l->M;
-    const int n_parts = (int)ceil_div<int64_t>(n, kSumRows);
-    const dim3 grid((unsigned)ceil_div<int64_t>(n_out, 64), (unsigned)std::min(n_parts, 65535), (unsigned)l->M);
+    const int n_parts = make_sweep(l->M, n, n_out).row_blocks;
     const unsigned totals = (unsigned)std::min<int64_t>(ceil_div<int64_t>((int64_t)l->M * n_out, kElementThreads), 4096);
-    if (f32) {
-      OP_DO(launch(s, column_sums_kernel<float>, grid, kElementThreads, 0, 1, j, room.sums, n_parts, s.clear ? s.error : nullptr));
+    if (f32)
       OP_DO(launch(s, column_totals_kernel<float>, dim3(totals), kElementThreads, 0, 1, (const float*)room.sums, n_parts, (int)n_out, (int)l->M,
                    (float*)l->dbias.data, l->dbias.worker_stride));
-    } else {
-      OP_DO(launch(s, column_sums_kernel<__nv_bfloat16>, grid, kElementThreads, 0, 1, j, room.sums, n_parts, s.clear ? s.error : nullptr));
+    else
       OP_DO(launch(s, column_totals_kernel<__nv_bfloat16>, dim3(totals), kElementThreads, 0, 1, (const float*)room.sums, n_parts, (int)n_out, (int)l->M,
                    (__nv_bfloat16*)l->dbias.data, l->dbias.worker_stride));
-    }
-    s.clear = false;
   }
   if (!l->dx.data && !l->dweight.data) {
     if (s.clear) OP_CUDA(cudaMemsetAsync(l->workspace, 0, 4, s.stream));
@@ -766,16 +771,16 @@ int run_schulz(Stream& s, std::vector<SchulzGroup>& groups, int steps, int plane
 
 int check_orthogonal_sizes(int32_t count, int64_t rows, int64_t cols, int32_t storage) {
   OP_DO(check_storage(storage));
-  const int64_t limit = (int64_t)1 << 31;
+  const int64_t limit = (int64_t)1 << 31, most = (int64_t)1 << 30;
   if (count < 1 || count > 1 << 20) return fail_op(NETMAX_INVALID_ARG, "count = %d outside [1, 2^20]", count);
-  if (rows < 1 || cols < 1 || rows >= limit || cols >= limit || rows * cols >= limit)
-    return fail_op(NETMAX_INVALID_ARG, "rows = %lld, cols = %lld: both must be positive and their product below 2^31", (long long)rows, (long long)cols);
+  if (rows < 1 || cols < 1 || rows > most || cols > most || rows * cols >= limit)
+    return fail_op(NETMAX_INVALID_ARG, "rows = %lld, cols = %lld: both must be positive, at most 2^30, and their product below 2^31", (long long)rows, (long long)cols);
   return NETMAX_OK;
 }
 struct OrthogonalRoom {
   SchulzGroup group;
   double* parts;
-  int pieces;
+  Sweep sweep;
   size_t total;
 };
 OrthogonalRoom orthogonal_room(void* workspace, int count, int64_t rows, int64_t cols, int storage) {
@@ -783,8 +788,8 @@ OrthogonalRoom orthogonal_room(void* workspace, int count, int64_t rows, int64_t
   Carver c(workspace);
   r.group.set(rows, cols, count);
   r.group.take(c, planes_of(storage));
-  r.pieces = (int)ceil_div<int64_t>(rows * cols, kPiece);
-  r.parts = (double*)c.take((size_t)count * r.pieces * sizeof(double));
+  r.sweep = make_sweep(count, rows, cols);
+  r.parts = (double*)c.take((size_t)count * blocks_of(r.sweep) * sizeof(double));
   r.total = c.used;
   return r;
 }
@@ -824,10 +829,7 @@ int netmax_orthogonalise(const netmax_orthogonal* o) try {
   np.u = o->u.data;
   np.row = o->u.row_stride;
   np.batch = o->u.worker_stride;
-  np.rows = (int32_t)o->rows;
-  np.cols = (int32_t)o->cols;
-  np.count = o->count;
-  np.pieces = room.pieces;
+  np.sweep = room.sweep;
   np.parts = room.parts;
   np.planes = q.x[0];
   np.dst_row = q.x_row;
@@ -836,7 +838,7 @@ int netmax_orthogonalise(const netmax_orthogonal* o) try {
   np.error = s.error;
   np.clear_error = 1;
   s.clear = false;
-  const dim3 grid((unsigned)room.pieces, (unsigned)std::min(o->count, 32768));
+  const dim3 grid((unsigned)blocks_of(room.sweep), (unsigned)std::min(o->count, 32768));
   OP_DO(launch(s, f32 ? norm_parts_kernel<float> : norm_parts_kernel<__nv_bfloat16>, grid, kElementThreads, 0, 1, np));
   OP_DO(launch(s, f32 ? first_iterate_kernel<float> : first_iterate_kernel<__nv_bfloat16>, grid, kElementThreads, 0, 1, np));
   OP_DO(q.encode_maps(planes_of(o->storage)));
@@ -900,7 +902,7 @@ int plan_step(int32_t M, int64_t d, const netmax_matrix* matrices, int32_t n, in
   auto add = [&](int64_t length, int matrix) {
     if (length == 0) return;
     plan.segments.push_back({plan.pieces, (uint32_t)at, (uint32_t)length, matrix});
-    plan.pieces += (uint32_t)ceil_div<int64_t>(length, kPiece);
+    plan.pieces += (uint32_t)ceil_div<int64_t>((at & 7) + length, kPiece);
     at += length;
   };
   for (int k : by_offset) {

@@ -6,9 +6,8 @@
 namespace netmax {
 
 constexpr int kElementThreads = 256;
-constexpr int kMaxParts = 64;       // partial maxima of a matrix
-constexpr int kPiece = 4096;        // elements of a replica that one CTA of the step's kernels works on
-constexpr int kSumRows = 256;       // rows of a part of a column sum
+constexpr int kPiece = 8192;        // elements of a replica that one CTA of the step's kernels works on
+constexpr int kUnroll = 4;          // rows that a thread has in flight
 
 __device__ __forceinline__ double block_sum(double v) {
   __shared__ double parts[kElementThreads / 32];
@@ -35,107 +34,170 @@ __device__ __forceinline__ float block_max(float v) {
   return s;
 }
 
+// How the elementwise kernels go over a matrix: a thread takes eight neighbouring columns, `1 << shift` threads a row, and a CTA
+// `rows_per_block` rows of a tile that wide.
+struct Sweep {
+  int32_t rows = 0, cols = 0, count = 0;
+  int32_t shift = 0, col_tiles = 1, row_blocks = 1, rows_per_block = 1;
+};
+struct SweepAt {
+  int col, count, row, last, step, row_block;  // `count` live columns from `col` on; rows row, row + step, ... below last
+};
+__device__ __forceinline__ SweepAt sweep_at(const Sweep& s, int block) {
+  SweepAt a;
+  const int lane = threadIdx.x & ((1 << s.shift) - 1);
+  a.row_block = block / s.col_tiles;
+  a.col = (((block - a.row_block * s.col_tiles) << s.shift) + lane) * 8;
+  a.count = min(8, s.cols - a.col);
+  a.step = kElementThreads >> s.shift;
+  a.row = a.row_block * s.rows_per_block + ((int)threadIdx.x >> s.shift);
+  a.last = min(s.rows, (a.row_block + 1) * s.rows_per_block);
+  return a;
+}
+
 // An operand on its way to the tensor cores: `count` matrices of rows x cols; with z, dy act'(z).
 struct OperandJob {
+  Sweep sweep;
   const void* src = nullptr;
   int64_t row = 0, batch = 0;
   const void* z = nullptr;
   int64_t z_row = 0, z_batch = 0;
   int32_t activation = 0;
-  int32_t rows = 0, cols = 0, count = 0, parts = 0;
-  void* dst = nullptr;
+  void* dst = nullptr;  // NULL: not laid out
   int64_t dst_row = 0, dst_batch = 0, dst_plane = 0;
-  float* maxima = nullptr;  // [count][parts]
+  float* maxima = nullptr;  // [count][blocks]
   int32_t* exponent = nullptr;
+  float* sums = nullptr;    // [count][row blocks][cols]: column sums of the blocks; NULL: not wanted
 };
 struct OperandParams {
-  OperandJob job[3];
+  OperandJob job[4];
   unsigned int* error = nullptr;
   int32_t clear_error = 0;
 };
 
 template <typename T>
-__device__ __forceinline__ float operand_value(const OperandJob& j, int q, uint32_t row, uint32_t col) {
-  float v = (float)((const T*)j.src)[q * j.batch + row * j.row + col];
-  if (j.z) v *= activation_slope((float)((const T*)j.z)[q * j.z_batch + row * j.z_row + col], j.activation);
-  return v;
+__device__ __forceinline__ void operand_values(const OperandJob& j, int q, int row, int col, int count, float (&v)[8]) {
+  load8((const T*)j.src + q * j.batch + row * j.row + col, count, v);
+  if (!j.z) return;
+  float z[8];
+  load8((const T*)j.z + q * j.z_batch + row * j.z_row + col, count, z);
+  if (j.activation == kActRelu) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] *= activation_slope(z[k], kActRelu);
+  } else if (j.activation == kActGelu) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] *= activation_slope(z[k], kActGelu);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] *= activation_slope(z[k], kActSilu);
+  }
 }
 
-// Largest finite magnitude of every matrix, in parts.
+// A block's column sums: every thread's rows first, then the threads of a column in order.
+__device__ __forceinline__ void write_sums(const OperandJob& j, const SweepAt& a, int q, const float (&sum)[8]) {
+  __shared__ float parts[kElementThreads * 8];
+  const int width = 8 << j.sweep.shift, lane = threadIdx.x & ((1 << j.sweep.shift) - 1);
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 8; ++k) parts[((int)threadIdx.x >> j.sweep.shift) * width + lane * 8 + k] = sum[k];
+  __syncthreads();
+  const int tile = a.col - lane * 8;
+  for (int c = threadIdx.x; c < width && tile + c < j.sweep.cols; c += kElementThreads) {
+    float s = 0.0f;
+    for (int r = 0; r < a.step; ++r) s += parts[r * width + c];
+    j.sums[((int64_t)q * j.sweep.row_blocks + a.row_block) * j.sweep.cols + tile + c] = s;
+  }
+}
+
+// fp32: the largest finite magnitude of every block, and the column sums.
 __global__ __launch_bounds__(kElementThreads) void operand_maxima_kernel(const __grid_constant__ OperandParams p) {
   ptx::let_successor_start();
   ptx::wait_for_predecessor();
   if (p.clear_error && blockIdx.x + blockIdx.y + blockIdx.z == 0 && threadIdx.x == 0) *p.error = 0;
   const OperandJob& j = p.job[blockIdx.z];
-  if ((int)blockIdx.x >= j.parts) return;
-  const uint32_t total = (uint32_t)j.rows * (uint32_t)j.cols, cols = (uint32_t)j.cols;
-  for (int q = blockIdx.y; q < j.count; q += gridDim.y) {
-    float most = 0.0f;
-    for (uint32_t e = blockIdx.x * kElementThreads + threadIdx.x; e < total; e += (uint32_t)j.parts * kElementThreads) {
-      const uint32_t row = e / cols;
-      const float v = fabsf(operand_value<float>(j, q, row, e - row * cols));
-      if (v <= 3.402823466e38f) most = fmaxf(most, v);
+  const int blocks = j.sweep.col_tiles * j.sweep.row_blocks;
+  if ((int)blockIdx.x >= blocks) return;
+  const SweepAt a = sweep_at(j.sweep, blockIdx.x);
+  for (int q = blockIdx.y; q < j.sweep.count; q += gridDim.y) {
+    float most = 0.0f, sum[8] = {};
+    if (a.count > 0) {
+      for (int row = a.row; row < a.last; row += kUnroll * a.step) {
+        float v[kUnroll][8];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          if (row + u * a.step < a.last) operand_values<float>(j, q, row + u * a.step, a.col, a.count, v[u]);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          if (row + u * a.step >= a.last) break;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float m = fabsf(v[u][k]);
+            if (m <= 3.402823466e38f) most = fmaxf(most, m);
+            sum[k] += v[u][k];
+          }
+        }
+      }
     }
-    most = block_max(most);
-    if (threadIdx.x == 0) j.maxima[q * j.parts + blockIdx.x] = most;
+    if (j.sums) write_sums(j, a, q, sum);
+    if (j.maxima) {
+      most = block_max(most);
+      if (threadIdx.x == 0) j.maxima[q * blocks + blockIdx.x] = most;
+    }
   }
 }
 
-// fp32 as two fp16 planes of the values times a power of two that brings the largest to [2^14, 2^15); bfloat16 as it is.
+// fp32 as two fp16 planes of the values times a power of two that brings the largest to [2^14, 2^15); bfloat16 as it is, with the
+// column sums.
 template <typename T>
 __global__ __launch_bounds__(kElementThreads) void operand_kernel(const __grid_constant__ OperandParams p) {
   ptx::let_successor_start();
   ptx::wait_for_predecessor();
   if (p.clear_error && blockIdx.x + blockIdx.y + blockIdx.z == 0 && threadIdx.x == 0) *p.error = 0;
   const OperandJob& j = p.job[blockIdx.z];
-  const uint32_t total = (uint32_t)j.rows * (uint32_t)j.cols, cols = (uint32_t)j.cols;
-  for (int q = blockIdx.y; q < j.count; q += gridDim.y) {
+  const int blocks = j.sweep.col_tiles * j.sweep.row_blocks;
+  if ((int)blockIdx.x >= blocks || (sizeof(T) == 4 && !j.dst)) return;
+  const SweepAt a = sweep_at(j.sweep, blockIdx.x);
+  for (int q = blockIdx.y; q < j.sweep.count; q += gridDim.y) {
     int exponent = 0;
     if (sizeof(T) == 4) {
       float most = 0.0f;
-      for (int k = threadIdx.x; k < j.parts; k += kElementThreads) most = fmaxf(most, j.maxima[q * j.parts + k]);
+      for (int k = threadIdx.x; k < blocks; k += kElementThreads) most = fmaxf(most, j.maxima[q * blocks + k]);
       most = block_max(most);
       if (most > 0.0f) exponent = min(14 - ilogbf(most), 126);  // (from 2^-112 on the largest lies lower; such values vanish beside any bias)
       if (blockIdx.x == 0 && threadIdx.x == 0) j.exponent[q] = exponent;
     }
     const float scale = ldexpf(1.0f, exponent);
-    for (uint32_t e = blockIdx.x * kElementThreads + threadIdx.x; e < total; e += gridDim.x * kElementThreads) {
-      const uint32_t row = e / cols, col = e - row * cols;
-      const float v = operand_value<T>(j, q, row, col);
-      const int64_t at = q * j.dst_batch + row * j.dst_row + col;
-      if (sizeof(T) == 4) {
-        __half hi, lo;
-        split(v * scale, hi, lo);
-        ((__half*)j.dst)[at] = hi;
-        ((__half*)j.dst)[at + j.dst_plane] = lo;
-      } else {
-        ((__nv_bfloat16*)j.dst)[at] = __float2bfloat16_rn(v);
+    float sum[8] = {};
+    if (a.count > 0) {
+      for (int row = a.row; row < a.last; row += kUnroll * a.step) {
+        float v[kUnroll][8];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          if (row + u * a.step < a.last) operand_values<T>(j, q, row + u * a.step, a.col, a.count, v[u]);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          if (row + u * a.step >= a.last) break;
+          const int64_t at = q * j.dst_batch + (row + u * a.step) * j.dst_row + a.col;  // (rows are padded to eight columns)
+          if (sizeof(T) == 4) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[u][k] *= scale;
+            uint4 hi, lo;
+            split8(v[u], hi, lo);
+            *(uint4*)((__half*)j.dst + at) = hi;
+            *(uint4*)((__half*)j.dst + at + j.dst_plane) = lo;
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[k] += v[u][k];
+            if (j.dst) store8((__nv_bfloat16*)j.dst + at, 8, v[u]);
+          }
+        }
       }
     }
+    if (sizeof(T) == 2 && j.sums) write_sums(j, a, q, sum);
   }
 }
 
-// Column sums of dy act'(z): parts of kSumRows rows each, 64 columns per CTA, four rows at a time.
-template <typename T>
-__global__ __launch_bounds__(kElementThreads) void column_sums_kernel(const __grid_constant__ OperandJob j, float* parts, int n_parts, unsigned int* clear) {
-  __shared__ float sums[4][64];
-  ptx::let_successor_start();
-  ptx::wait_for_predecessor();
-  if (clear && blockIdx.x + blockIdx.y + blockIdx.z == 0 && threadIdx.x == 0) *clear = 0;
-  const int lane = threadIdx.x % 64, group = threadIdx.x / 64, col = blockIdx.x * 64 + lane;
-  for (int q = blockIdx.z; q < j.count; q += gridDim.z) {
-    for (int part = blockIdx.y; part < n_parts; part += gridDim.y) {
-      const int first = part * kSumRows, last = min(j.rows, first + kSumRows);
-      float s = 0.0f;
-      if (col < j.cols)
-        for (int row = first + group; row < last; row += 4) s += operand_value<T>(j, q, row, col);
-      sums[group][lane] = s;
-      __syncthreads();
-      if (group == 0 && col < j.cols) parts[((int64_t)q * n_parts + part) * j.cols + col] = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
-      __syncthreads();
-    }
-  }
-}
+// The blocks' column sums added up, in double.
 template <typename T>
 __global__ __launch_bounds__(kElementThreads) void column_totals_kernel(const float* parts, int n_parts, int cols, int count, T* out, int64_t batch) {
   ptx::let_successor_start();
@@ -150,27 +212,27 @@ __global__ __launch_bounds__(kElementThreads) void column_totals_kernel(const fl
 }
 
 // ---- Newton-Schulz: norms and the first iterate ------------------------------------------------
-struct NormParams {  // `count` matrices of rows x cols on their own
+struct NormParams {  // matrices on their own
+  Sweep sweep;
   const void* u = nullptr;
   int64_t row = 0, batch = 0;
-  int32_t rows = 0, cols = 0, count = 0, pieces = 0;
-  double* parts = nullptr;  // [count][pieces] sums of squares
+  double* parts = nullptr;  // [count][blocks] sums of squares
   __half* planes = nullptr;
   int64_t dst_row = 0, dst_batch = 0, dst_plane = 0;
   unsigned int* error = nullptr;
   int32_t clear_error = 0;
 };
-__device__ __forceinline__ void first_iterate(float u, double inverse, __half* at, int64_t plane) {
-  __half hi, lo;
-  split((float)((double)u * inverse), hi, lo);
-  at[0] = hi;
-  at[plane] = lo;
-}
-// 2^14 / norm; 0 for a matrix of zeros.  A norm that is not finite makes the whole matrix NaN, as the products would.
-__device__ __forceinline__ double inverse_norm(double squares) {
-  if (squares == 0.0) return 0.0;
-  if (!(squares <= 1.7e308)) return squares - squares;
-  return (double)kPlaneScale / sqrt(squares);
+// 2^14 / norm as two factors, so that neither they nor the product with one of them leave fp32's range where the iterate does not; zeros
+// for a matrix of zeros.  A norm that is not finite makes the whole matrix NaN, as the products would.
+struct Inverse {
+  float a, b;
+};
+__device__ __forceinline__ Inverse inverse_norm(double squares) {
+  if (squares == 0.0) return {0.0f, 0.0f};
+  if (!(squares <= 1.7e308)) return {__int_as_float(0x7FC00000), 1.0f};
+  const double inverse = (double)kPlaneScale / sqrt(squares);
+  const int e = ilogb(inverse) / 2;
+  return {ldexpf(1.0f, e), (float)ldexp(inverse, -e)};
 }
 
 template <typename T>
@@ -178,32 +240,53 @@ __global__ __launch_bounds__(kElementThreads) void norm_parts_kernel(const __gri
   ptx::let_successor_start();
   ptx::wait_for_predecessor();
   if (p.clear_error && blockIdx.x + blockIdx.y == 0 && threadIdx.x == 0) *p.error = 0;
-  const uint32_t total = (uint32_t)p.rows * (uint32_t)p.cols, cols = (uint32_t)p.cols;
-  for (int q = blockIdx.y; q < p.count; q += gridDim.y) {
+  const SweepAt a = sweep_at(p.sweep, blockIdx.x);
+  for (int q = blockIdx.y; q < p.sweep.count; q += gridDim.y) {
     double s = 0.0;
-    const uint32_t first = blockIdx.x * kPiece, last = min(total, first + kPiece);
-    for (uint32_t e = first + threadIdx.x; e < last; e += kElementThreads) {
-      const uint32_t row = e / cols;
-      const double v = (double)(float)((const T*)p.u)[q * p.batch + row * p.row + (e - row * cols)];
-      s += v * v;
+    if (a.count > 0) {
+      for (int row = a.row; row < a.last; row += kUnroll * a.step) {
+        float v[kUnroll][8];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          if (row + u * a.step < a.last) load8((const T*)p.u + q * p.batch + (row + u * a.step) * p.row + a.col, a.count, v[u]);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          if (row + u * a.step >= a.last) break;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s += (double)v[u][k] * (double)v[u][k];
+        }
+      }
     }
     s = block_sum(s);
-    if (threadIdx.x == 0) p.parts[(int64_t)q * p.pieces + blockIdx.x] = s;
+    if (threadIdx.x == 0) p.parts[(int64_t)q * gridDim.x + blockIdx.x] = s;
   }
 }
 template <typename T>
 __global__ __launch_bounds__(kElementThreads) void first_iterate_kernel(const __grid_constant__ NormParams p) {
   ptx::let_successor_start();
   ptx::wait_for_predecessor();
-  const uint32_t total = (uint32_t)p.rows * (uint32_t)p.cols, cols = (uint32_t)p.cols;
-  for (int q = blockIdx.y; q < p.count; q += gridDim.y) {
+  const SweepAt a = sweep_at(p.sweep, blockIdx.x);
+  for (int q = blockIdx.y; q < p.sweep.count; q += gridDim.y) {
     double s = 0.0;
-    for (int k = threadIdx.x; k < p.pieces; k += kElementThreads) s += p.parts[(int64_t)q * p.pieces + k];
-    const double inverse = inverse_norm(block_sum(s));
-    const uint32_t first = blockIdx.x * kPiece, last = min(total, first + kPiece);
-    for (uint32_t e = first + threadIdx.x; e < last; e += kElementThreads) {
-      const uint32_t row = e / cols, col = e - row * cols;
-      first_iterate((float)((const T*)p.u)[q * p.batch + row * p.row + col], inverse, p.planes + q * p.dst_batch + row * p.dst_row + col, p.dst_plane);
+    for (int k = threadIdx.x; k < (int)gridDim.x; k += kElementThreads) s += p.parts[(int64_t)q * gridDim.x + k];
+    const Inverse inverse = inverse_norm(block_sum(s));
+    if (a.count <= 0) continue;
+    for (int row = a.row; row < a.last; row += kUnroll * a.step) {
+      float v[kUnroll][8];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u)
+        if (row + u * a.step < a.last) load8((const T*)p.u + q * p.batch + (row + u * a.step) * p.row + a.col, a.count, v[u]);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        if (row + u * a.step >= a.last) break;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[u][k] = v[u][k] * inverse.a * inverse.b;
+        uint4 hi, lo;
+        split8(v[u], hi, lo);
+        __half* at = p.planes + q * p.dst_batch + (row + u * a.step) * p.dst_row + a.col;
+        *(uint4*)at = hi;
+        *(uint4*)(at + p.dst_plane) = lo;
+      }
     }
   }
 }
@@ -246,6 +329,35 @@ __device__ __forceinline__ int find_segment(const StepParams& p, uint32_t piece)
   return lo;
 }
 
+// A piece of a segment: elements [first, last), taken eight at a time from the multiple of eight at or before `first` on, so that every
+// full group lies on a 16-byte boundary where the arrays do.
+struct Piece {
+  uint32_t first, last, group;
+};
+__device__ __forceinline__ Piece piece_of(const StepSegment& s, uint32_t block) {
+  Piece p;
+  const uint32_t base = s.offset & ~7u, begin = base + (block - s.first_piece) * kPiece;
+  p.first = max(begin, s.offset);
+  p.last = min(begin + kPiece, s.offset + s.length);
+  p.group = begin + threadIdx.x * 8;
+  return p;
+}
+// Eight elements from `at` on, of which those in [first, last) exist.
+template <typename T>
+__device__ __forceinline__ void load_group(const T* base, uint32_t at, const Piece& p, float (&v)[8]) {
+  if (at >= p.first && at + 8 <= p.last) return load8(base + at, 8, v);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = at + k >= p.first && at + k < p.last ? (float)base[at + k] : 0.0f;
+}
+template <typename T>
+__device__ __forceinline__ void store_group(T* base, uint32_t at, const Piece& p, const float (&v)[8]) {
+  if (at >= p.first && at + 8 <= p.last) return store8(base + at, 8, v);
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (at + k >= p.first && at + k < p.last) base[at + k] = (T)v[k];
+}
+constexpr int kGroupsPerThread = kPiece / (8 * kElementThreads);
+
 // m' = mu m + g, u = g + mu m' or m'; sums of squares of u inside matrices, the whole update outside them.
 template <typename T>
 __global__ __launch_bounds__(kElementThreads) void step_momentum_kernel(const __grid_constant__ StepParams p) {
@@ -253,32 +365,56 @@ __global__ __launch_bounds__(kElementThreads) void step_momentum_kernel(const __
   ptx::wait_for_predecessor();
   if (p.clear_error && blockIdx.x + blockIdx.y == 0 && threadIdx.x == 0) *p.error = 0;
   const StepSegment seg = p.segment[find_segment(p, blockIdx.x)];
-  const uint32_t first = seg.offset + (blockIdx.x - seg.first_piece) * kPiece, last = min(seg.offset + seg.length, first + kPiece);
+  const Piece piece = piece_of(seg, blockIdx.x);
   for (int i = blockIdx.y; i < p.workers; i += gridDim.y) {
     const T* g = (const T*)p.gradient + i * p.gradient_row;
     const float* m = p.momentum + i * p.momentum_row;
     float* m_next = p.momentum_next + i * p.momentum_next_row;
+    double s = 0.0;
+    float grad[kGroupsPerThread][8], mom[kGroupsPerThread][8];
+#pragma unroll
+    for (int u = 0; u < kGroupsPerThread; ++u) {
+      const uint32_t at = piece.group + u * 8 * kElementThreads;
+      if (at >= piece.last) break;
+      load_group(g, at, piece, grad[u]);
+      load_group(m, at, piece, mom[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kGroupsPerThread; ++u) {
+      const uint32_t at = piece.group + u * 8 * kElementThreads;
+      if (at >= piece.last) break;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        mom[u][k] = fmaf(p.mu, mom[u][k], grad[u][k]);
+        grad[u][k] = p.nesterov ? fmaf(p.mu, mom[u][k], grad[u][k]) : mom[u][k];  // (elements outside the piece are zeros)
+        s += (double)grad[u][k] * (double)grad[u][k];
+      }
+      store_group(m_next, at, piece, mom[u]);
+    }
+    if (seg.matrix >= 0) {
+      s = block_sum(s);
+      if (threadIdx.x == 0) p.parts[(int64_t)i * p.pieces + blockIdx.x] = s;
+      continue;
+    }
     const int peer = p.pull.peers[i * p.pull.draw_stride];
     const bool pull = peer != i && (uint32_t)peer < (uint32_t)p.workers;
     const float w = pull ? p.pull.weights[i * p.pull.draw_stride] : 0.0f;
     const T* own = (const T*)p.pull.x + i * p.pull.x_row;
     const T* other = (const T*)p.pull.x + (pull ? peer : i) * p.pull.x_row;
     T* next = (T*)p.pull.x_next + i * p.pull.next_row;
-    double s = 0.0;
-    for (uint32_t e = first + threadIdx.x; e < last; e += kElementThreads) {
-      const float grad = (float)g[e], after = fmaf(p.mu, m[e], grad);
-      m_next[e] = after;
-      const float u = p.nesterov ? fmaf(p.mu, after, grad) : after;
-      if (seg.matrix >= 0) {
-        s += (double)u * (double)u;
-      } else {
-        const float x = (float)own[e], h = fmaf(-p.pull.lr, fmaf(p.pull.decay, x, u), x);
-        next[e] = (T)(pull ? fmaf(-w, h - (float)other[e], h) : h);
+#pragma unroll
+    for (int u = 0; u < kGroupsPerThread; ++u) {
+      const uint32_t at = piece.group + u * 8 * kElementThreads;
+      if (at >= piece.last) break;
+      float x[8], xm[8];
+      load_group(own, at, piece, x);
+      load_group(other, at, piece, xm);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float h = fmaf(-p.pull.lr, fmaf(p.pull.decay, x[k], grad[u][k]), x[k]);
+        x[k] = pull ? fmaf(-w, h - xm[k], h) : h;
       }
-    }
-    if (seg.matrix >= 0) {
-      s = block_sum(s);
-      if (threadIdx.x == 0) p.parts[(int64_t)i * p.pieces + blockIdx.x] = s;
+      store_group(next, at, piece, x);
     }
   }
 }
@@ -286,22 +422,56 @@ template <typename T>
 __global__ __launch_bounds__(kElementThreads) void step_first_iterate_kernel(const __grid_constant__ StepParams p, const __grid_constant__ StepIterateParams tables) {
   ptx::let_successor_start();
   ptx::wait_for_predecessor();
-  const int at = find_segment(p, blockIdx.x);
-  const StepSegment seg = p.segment[at];
+  const StepSegment seg = p.segment[find_segment(p, blockIdx.x)];
   if (seg.matrix < 0) return;
   const StepMatrix& to = tables.matrix[seg.matrix];
-  const uint32_t pieces = (seg.length + kPiece - 1) / kPiece;
-  const uint32_t begin = (blockIdx.x - seg.first_piece) * kPiece, end = min(seg.length, begin + kPiece), cols = to.cols;
+  const Piece piece = piece_of(seg, blockIdx.x);
+  const uint32_t pieces = ((seg.offset & 7) + seg.length + kPiece - 1) / kPiece, cols = to.cols;
+  const bool whole = ((seg.offset | cols) & 7) == 0;  // groups of eight do not cross rows
   for (int i = blockIdx.y; i < p.workers; i += gridDim.y) {
+    const T* g = (const T*)p.gradient + i * p.gradient_row;
+    const float* m_next = p.momentum_next + i * p.momentum_next_row;
+    float grad[kGroupsPerThread][8], mom[kGroupsPerThread][8];
+#pragma unroll
+    for (int u = 0; u < kGroupsPerThread; ++u) {
+      const uint32_t at = piece.group + u * 8 * kElementThreads;
+      if (at >= piece.last) break;
+      load_group(m_next, at, piece, mom[u]);
+      if (p.nesterov) load_group(g, at, piece, grad[u]);
+    }
     double s = 0.0;
     for (uint32_t k = threadIdx.x; k < pieces; k += kElementThreads) s += p.parts[(int64_t)i * p.pieces + seg.first_piece + k];
-    const double inverse = inverse_norm(block_sum(s));
-    const T* g = (const T*)p.gradient + i * p.gradient_row + seg.offset;
-    const float* m_next = p.momentum_next + i * p.momentum_next_row + seg.offset;
-    for (uint32_t e = begin + threadIdx.x; e < end; e += kElementThreads) {
-      const float after = m_next[e], u = p.nesterov ? fmaf(p.mu, after, (float)g[e]) : after;
-      const uint32_t row = e / cols;
-      first_iterate(u, inverse, to.planes + i * to.worker + row * to.row + (e - row * cols), to.plane);
+    const Inverse inverse = inverse_norm(block_sum(s));
+    __half* planes = to.planes + i * to.worker;
+#pragma unroll
+    for (int u = 0; u < kGroupsPerThread; ++u) {
+      const uint32_t at = piece.group + u * 8 * kElementThreads;
+      if (at >= piece.last) break;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) mom[u][k] = (p.nesterov ? fmaf(p.mu, mom[u][k], grad[u][k]) : mom[u][k]) * inverse.a * inverse.b;
+      uint4 hi, lo;
+      split8(mom[u], hi, lo);
+      if (whole) {  // (then the piece's ends are multiples of eight, too)
+        const uint32_t e = at - seg.offset, row = e / cols;
+        __half* to8 = planes + row * to.row + (e - row * cols);
+        *(uint4*)to8 = hi;
+        *(uint4*)(to8 + to.plane) = lo;
+      } else {
+        const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
+        const uint32_t begin = max(at, piece.first) - seg.offset;
+        uint32_t row = begin / cols, col = begin - row * cols;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (at + k < piece.first || at + k >= piece.last) continue;
+          __half* to1 = planes + row * to.row + col;
+          to1[0] = __ushort_as_half((unsigned short)(h[k / 2] >> (16 * (k % 2))));
+          to1[to.plane] = __ushort_as_half((unsigned short)(l[k / 2] >> (16 * (k % 2))));
+          if (++col == cols) {
+            col = 0;
+            ++row;
+          }
+        }
+      }
     }
   }
 }
