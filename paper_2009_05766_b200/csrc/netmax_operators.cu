@@ -15,6 +15,7 @@
 #include "netmax_operators.cuh"
 #include "netmax_operators.h"
 #include "netmax_policy.h"
+#include "netmax_small.cuh"
 
 using namespace netmax;
 
@@ -793,6 +794,18 @@ OrthogonalRoom orthogonal_room(void* workspace, int count, int64_t rows, int64_t
   r.total = c.used;
   return r;
 }
+// Matrices that one CTA each orthogonalises.
+int run_small(Stream& s, SmallParams& p, unsigned blocks, size_t smem, uint32_t tmem_columns, void (*kernel)(const SmallParams)) {
+  p.tmem_columns = tmem_columns;
+  p.ca = kA;
+  p.cb = kB;
+  p.cc = kC;
+  p.error = s.error;
+  p.clear_error = s.clear;
+  s.clear = false;
+  OP_CUDA(raise_smem_limit((const void*)kernel, smem));
+  return launch(s, kernel, dim3(blocks), kSmallThreads, smem, 1, p);
+}
 int check_steps(int steps) {
   if (steps < 1 || steps > 20) return fail_op(NETMAX_INVALID_ARG, "steps = %d outside [1, 20]", steps);
   return NETMAX_OK;
@@ -824,6 +837,20 @@ int netmax_orthogonalise(const netmax_orthogonal* o) try {
   if (!on.ok) return fail_op(NETMAX_CUDA_ERROR, "cudaSetDevice failed");
   Stream s{(cudaStream_t)o->stream, (unsigned int*)o->workspace};
   const bool f32 = o->storage == NETMAX_STORAGE_F32;
+  if (is_small(o->rows, o->cols)) {
+    SmallParams sp;
+    sp.u = o->u.data;
+    sp.row = o->u.row_stride;
+    sp.batch = o->u.worker_stride;
+    sp.out = o->out.data;
+    sp.out_row = o->out.row_stride;
+    sp.out_batch = o->out.worker_stride;
+    sp.rows = (int32_t)o->rows;
+    sp.cols = (int32_t)o->cols;
+    sp.steps = o->steps;
+    return run_small(s, sp, (unsigned)o->count, small_smem((uint32_t)o->rows, (uint32_t)o->cols), small_tmem((uint32_t)o->rows, (uint32_t)o->cols),
+                     f32 ? small_schulz_kernel<float, false> : small_schulz_kernel<__nv_bfloat16, false>);
+  }
   SchulzGroup& q = room.group;
   NormParams np;
   np.u = o->u.data;
@@ -869,7 +896,8 @@ int netmax_workspace_status(const void* workspace, int32_t device, void* stream)
 namespace {
 
 struct StepPlan {
-  std::vector<netmax_matrix> sorted;   // by shape, then by offset: the order of the tables
+  std::vector<netmax_matrix> small;    // those that one CTA orthogonalises
+  std::vector<netmax_matrix> sorted;   // the others by shape, then by offset: the order of the tables
   std::vector<SchulzGroup> groups;     // of equal shapes
   std::vector<int> first;              // of a group, in `sorted`
   std::vector<StepSegment> segments;   // by offset
@@ -892,12 +920,17 @@ int plan_step(int32_t M, int64_t d, const netmax_matrix* matrices, int32_t n, in
     if (!std::isfinite(m.scale)) return fail_op(NETMAX_INVALID_ARG, "the scale of the matrix at %lld is not finite", (long long)m.offset);
     if ((int64_t)M * m.rows * m.cols >= (int64_t)1 << 40) return fail_op(NETMAX_INVALID_ARG, "M matrices of %lld x %lld are too many", (long long)m.rows, (long long)m.cols);
   }
+  const auto apart = std::stable_partition(plan.sorted.begin(), plan.sorted.end(), [](const netmax_matrix& m) { return !is_small(m.rows, m.cols); });
+  plan.small.assign(apart, plan.sorted.end());
+  plan.sorted.erase(apart, plan.sorted.end());
   std::sort(plan.sorted.begin(), plan.sorted.end(), [](const netmax_matrix& a, const netmax_matrix& b) {
     return std::tie(a.rows, a.cols, a.offset) < std::tie(b.rows, b.cols, b.offset);
   });
-  std::vector<int> by_offset(plan.sorted.size());
-  for (size_t k = 0; k < by_offset.size(); ++k) by_offset[k] = (int)k;
-  std::sort(by_offset.begin(), by_offset.end(), [&](int a, int b) { return plan.sorted[a].offset < plan.sorted[b].offset; });
+  const int others = (int)plan.sorted.size();
+  auto matrix = [&](int k) -> const netmax_matrix& { return k < others ? plan.sorted[k] : plan.small[k - others]; };
+  std::vector<int> by_offset((size_t)n);
+  for (int k = 0; k < n; ++k) by_offset[k] = k;
+  std::sort(by_offset.begin(), by_offset.end(), [&](int a, int b) { return matrix(a).offset < matrix(b).offset; });
   int64_t at = 0;
   auto add = [&](int64_t length, int matrix) {
     if (length == 0) return;
@@ -906,10 +939,11 @@ int plan_step(int32_t M, int64_t d, const netmax_matrix* matrices, int32_t n, in
     at += length;
   };
   for (int k : by_offset) {
-    const netmax_matrix& m = plan.sorted[k];
+    const netmax_matrix& m = matrix(k);
     if (m.offset < at) return fail_op(NETMAX_INVALID_ARG, "the matrix at %lld overlaps the one before it", (long long)m.offset);
     add(m.offset - at, -1);
-    add(m.rows * m.cols, k);
+    if (k < others) add(m.rows * m.cols, k);
+    else at += m.rows * m.cols;  // (its kernel takes the whole update)
   }
   add(d - at, -1);
   Carver c(workspace);
@@ -990,10 +1024,33 @@ int enqueue_step(const netmax_step& t, int draw_stride, unsigned int* error, int
   sp.pull.decay = (float)t.decay;
   sp.pull.workers = t.M;
   sp.error = s.error;
+  const dim3 grid(plan.pieces, (unsigned)t.M);
+  if (!plan.small.empty()) {
+    SmallParams mp;
+    mp.gradient = sp.gradient;
+    mp.gradient_row = sp.gradient_row;
+    mp.momentum = sp.momentum;
+    mp.momentum_next = sp.momentum_next;
+    mp.momentum_row = sp.momentum_row;
+    mp.momentum_next_row = sp.momentum_next_row;
+    mp.mu = sp.mu;
+    mp.nesterov = sp.nesterov;
+    mp.pull = sp.pull;
+    mp.steps = t.steps;
+    size_t smem = 0;
+    uint32_t columns = 0;
+    for (size_t k = 0; k < plan.small.size(); ++k) {
+      const netmax_matrix& m = plan.small[k];
+      mp.matrix[k] = {(uint32_t)m.offset, (uint32_t)m.rows, (uint32_t)m.cols, (float)m.scale};
+      smem = std::max(smem, small_smem((uint32_t)m.rows, (uint32_t)m.cols));
+      columns = std::max(columns, small_tmem((uint32_t)m.rows, (uint32_t)m.cols));
+    }
+    OP_DO(run_small(s, mp, (unsigned)plan.small.size() * (unsigned)t.M, smem, columns,
+                    f32 ? small_schulz_kernel<float, true> : small_schulz_kernel<__nv_bfloat16, true>));
+  }
   sp.clear_error = s.clear;
   s.clear = false;
-  const dim3 grid(plan.pieces, (unsigned)t.M);
-  OP_DO(launch(s, f32 ? step_momentum_kernel<float> : step_momentum_kernel<__nv_bfloat16>, grid, kElementThreads, 0, 1, sp));
+  if (plan.pieces > 0) OP_DO(launch(s, f32 ? step_momentum_kernel<float> : step_momentum_kernel<__nv_bfloat16>, grid, kElementThreads, 0, 1, sp));
   if (!plan.groups.empty()) {
     StepIterateParams tables;
     std::memset(&tables, 0, sizeof tables);

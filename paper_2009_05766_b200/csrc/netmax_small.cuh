@@ -1,0 +1,357 @@
+// Newton-Schulz orthogonalisation of small matrices (smaller side up to 64 with a larger one up to 512, or up to 128 and 256): a CTA per
+// matrix, everything in one launch.
+//
+// The general path is 15 products and two sweeps, each a launch of 5-7 us whose work is far below a microsecond for such sizes (four
+// 64 x 64 matrices: 112 us).  Here the iterate stays in shared memory as two fp16 planes in the tensor cores' own layout (blocks of 64
+// columns, rows of 128 bytes, 16-byte pieces swizzled by the row), S = X X^T and the polynomial beside it, accumulators in TMEM; a
+// step is three rounds of products, wait, 16 columns a thread, barrier.  The one layout serves as k-contiguous operand (X X^T, S S, P) and as
+// n-contiguous one (X in P X).  Tall matrices are transposed on their way in and out.  All products take the three terms of two-plane factors,
+// whatever the storage: they cost nothing here.  Sums over more than 128 columns of X go to accumulators of their own, added in fp32.
+#pragma once
+#include "netmax_operators.cuh"
+
+namespace netmax {
+
+constexpr int kSmallThreads = 512;
+
+struct SmallMatrix {
+  uint32_t offset, rows, cols;
+  float scale;
+};
+struct SmallParams {
+  // matrices on their own
+  const void* u = nullptr;
+  int64_t row = 0, batch = 0;
+  void* out = nullptr;
+  int64_t out_row = 0, out_batch = 0;
+  // or inside replicas: matrix blockIdx.x / workers of worker blockIdx.x % workers
+  const void* gradient = nullptr;
+  int64_t gradient_row = 0;
+  const float* momentum = nullptr;
+  float* momentum_next = nullptr;
+  int64_t momentum_row = 0, momentum_next_row = 0;
+  float mu = 0;
+  int32_t nesterov = 0;
+  PullParams pull;
+  SmallMatrix matrix[kMaxMatrices];
+  int32_t rows = 0, cols = 0, steps = 0;
+  uint32_t tmem_columns = 0;
+  float ca = 0, cb = 0, cc = 0;
+  unsigned int* error = nullptr;
+  int32_t clear_error = 0;
+};
+
+// Shared memory of a matrix: two planes of the iterate, two of S, and a block behind them (a product's 128 rows of A run past 64-row
+// blocks; what they find there reaches only rows of the accumulator that nobody reads).
+__host__ __device__ inline uint32_t small_side(uint32_t rows, uint32_t cols) { return (rows < cols ? rows : cols) <= 64 ? 64 : 128; }
+__host__ __device__ inline uint32_t small_length(uint32_t rows, uint32_t cols) { return ((rows < cols ? cols : rows) + 63) / 64 * 64; }
+__host__ __device__ inline bool is_small(int64_t rows, int64_t cols) {
+  const int64_t side = rows < cols ? rows : cols, length = rows < cols ? cols : rows;
+  return (side <= 64 && length <= 512) || (side <= 128 && length <= 256);
+}
+inline size_t small_smem(uint32_t rows, uint32_t cols) {
+  const size_t r = small_side(rows, cols), l = small_length(rows, cols);
+  return 1024 + 2 * r * l * 2 + 2 * r * r * 2 + kBoxBytes;
+}
+inline uint32_t small_tmem(uint32_t rows, uint32_t cols) {
+  const uint32_t r = small_side(rows, cols), l = small_length(rows, cols), need = l > (l + 127) / 128 * r ? l : (l + 127) / 128 * r;
+  uint32_t c = 32;
+  while (c < need) c *= 2;
+  return c;
+}
+
+__device__ __forceinline__ void tmem_load16(uint32_t at, float (&v)[16]) {
+  uint32_t r[16];
+  __syncwarp();
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(at));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ uint64_t small_descriptor(uint32_t at, uint32_t leading) {
+  return (uint64_t)((at & 0x3FFFF) >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// Byte of element (row, column) in a plane of `side` rows.
+__device__ __forceinline__ uint32_t small_at(uint32_t side, uint32_t row, uint32_t col) {
+  return (col / 64) * side * 128 + row * 128 + ((((col % 64) / 8) ^ (row & 7)) * 16) + (col % 8) * 2;
+}
+
+template <typename T, bool kStep>
+__global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __grid_constant__ SmallParams p) {
+  extern __shared__ unsigned char raw[];
+  __shared__ __align__(8) uint64_t bar;
+  __shared__ uint32_t tmem_at;
+  __shared__ double squares[kSmallThreads / 32];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  unsigned char* const base = raw + (((ptx::smem(raw) + 1023) & ~1023u) - ptx::smem(raw));
+  const int worker = kStep ? blockIdx.x % p.pull.workers : 0, which = kStep ? blockIdx.x / p.pull.workers : 0;
+  const uint32_t rows = kStep ? p.matrix[which].rows : (uint32_t)p.rows, cols = kStep ? p.matrix[which].cols : (uint32_t)p.cols;
+  const bool tall = rows > cols;
+  const uint32_t side = small_side(rows, cols), length = small_length(rows, cols);
+  const uint32_t x_plane = side * length * 2, s_plane = side * side * 2;
+  unsigned char* const x = base;
+  unsigned char* const s = base + 2 * x_plane;
+  if (threadIdx.x == 0) {
+    ptx::barrier_init(ptx::smem(&bar), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) ptx::tmem_alloc<1>(ptx::smem(&tmem_at), p.tmem_columns);
+  for (uint32_t at = threadIdx.x * 16; at < 2 * x_plane; at += kSmallThreads * 16) *(uint4*)(x + at) = make_uint4(0, 0, 0, 0);
+  ptx::let_successor_start();
+  ptx::wait_for_predecessor();
+  if (p.clear_error && blockIdx.x == 0 && threadIdx.x == 0) *p.error = 0;
+
+  // ---- the matrix, its norm, and the first iterate
+  const uint32_t groups_per_row = (cols + 7) / 8, groups = rows * groups_per_row;  // at most 4096 of eight columns
+  float u[8][8];
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t group = i * kSmallThreads + threadIdx.x;
+    if (group >= groups) break;
+    const uint32_t row = group / groups_per_row, col = (group - row * groups_per_row) * 8;
+    const int count = min(8u, cols - col);
+    if (kStep) {
+      const int64_t at = (int64_t)p.matrix[which].offset + row * cols + col;
+      float grad[8];
+      load8((const T*)p.gradient + worker * p.gradient_row + at, count, grad);
+      load8(p.momentum + worker * p.momentum_row + at, count, u[i]);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) u[i][k] = fmaf(p.mu, u[i][k], grad[k]);
+      store8(p.momentum_next + worker * p.momentum_next_row + at, count, u[i]);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (p.nesterov) u[i][k] = fmaf(p.mu, u[i][k], grad[k]);
+    } else {
+      load8((const T*)p.u + blockIdx.x * p.batch + row * p.row + col, count, u[i]);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += (double)u[i][k] * (double)u[i][k];  // (columns that are not there are zeros)
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  if (lane == 0) squares[warp] = sum;
+  ptx::fence_before();
+  __syncthreads();
+  ptx::fence_after();
+  const uint32_t tmem = tmem_at;
+  sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < kSmallThreads / 32; ++w) sum += squares[w];
+  const Inverse inverse = inverse_norm(sum);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t group = i * kSmallThreads + threadIdx.x;
+    if (group >= groups) break;
+    const uint32_t row = group / groups_per_row, col = (group - row * groups_per_row) * 8;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) u[i][k] = u[i][k] * inverse.a * inverse.b;
+    uint4 hi, lo;
+    split8(u[i], hi, lo);
+    if (!tall) {
+      *(uint4*)(x + small_at(side, row, col)) = hi;
+      *(uint4*)(x + x_plane + small_at(side, row, col)) = lo;
+    } else {
+      const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (col + k >= cols) break;
+        const uint32_t at = small_at(side, col + k, row);
+        *(unsigned short*)(x + at) = (unsigned short)(h[k / 2] >> (16 * (k % 2)));
+        *(unsigned short*)(x + x_plane + at) = (unsigned short)(l[k / 2] >> (16 * (k % 2)));
+      }
+    }
+  }
+
+  // ---- the steps
+  const uint32_t idesc = 1u << 4 | (128 / 16) << 24;  // fp16, sums in fp32, 128 rows
+  const uint32_t m = (warp % 4) * 32 + lane;          // this thread's row, and every fourth 16 columns
+  const uint32_t from = tmem + ((warp % 4) * 32 << 16);
+  const bool live = (warp % 4) * 32 < (int)side;
+  const uint32_t parts = (length + 127) / 128;
+  bool ok = true;
+  uint32_t phase = 0;
+  auto products_done = [&] {  // for all threads alike
+    ok = __syncthreads_and(ptx::wait(ptx::smem(&bar), phase & 1)) != 0;
+    ++phase;
+    ptx::fence_after();
+  };
+  auto written = [&] {  // what threads have stored is there for the tensor cores
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    ptx::fence_before();
+    __syncthreads();
+    ptx::fence_after();
+  };
+  written();
+  for (int step = 0; step < p.steps && ok; ++step) {
+    const bool last = step + 1 == p.steps;
+    if (warp == 0 && ptx::elect()) {  // S = X X^T
+      for (uint32_t part = 0; part < parts; ++part)
+        for (int term = 0; term < 3; ++term) {
+          const uint32_t a = ptx::smem(x) + (term == 1 ? x_plane : 0), b = ptx::smem(x) + (term == 0 ? x_plane : 0);
+          for (uint32_t k = part * 128; k < min(length, part * 128 + 128); k += 16) {
+            const uint32_t at = (k / 64) * side * 128 + (k % 64) * 2;
+            ptx::mma<1>(tmem + part * side, small_descriptor(a + at, 16), small_descriptor(b + at, 16), idesc | side / 8 << 17, term > 0 || k > part * 128);
+          }
+        }
+      ptx::commit<1>(ptx::smem(&bar));
+    }
+    __syncwarp();
+    products_done();
+    if (!ok) break;
+    if (live)
+      for (uint32_t c = (warp / 4) * 16; c < side; c += 64) {
+        float v[16], w[16];
+        tmem_load16(from + c, v);
+        for (uint32_t part = 1; part < parts; ++part) {
+          tmem_load16(from + part * side + c, w);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] += w[k];
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float t[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) t[k] = v[8 * h + k] * kPlaneUnscale;
+          uint4 hi, lo;
+          split8(t, hi, lo);
+          *(uint4*)(s + small_at(side, m, c + 8 * h)) = hi;
+          *(uint4*)(s + s_plane + small_at(side, m, c + 8 * h)) = lo;
+        }
+      }
+    written();
+    if (warp == 0 && ptx::elect()) {  // S S
+      for (int term = 0; term < 3; ++term) {
+        const uint32_t a = ptx::smem(s) + (term == 1 ? s_plane : 0), b = ptx::smem(s) + (term == 0 ? s_plane : 0);
+        for (uint32_t k = 0; k < side; k += 16) {
+          const uint32_t at = (k / 64) * side * 128 + (k % 64) * 2;
+          ptx::mma<1>(tmem, small_descriptor(a + at, 16), small_descriptor(b + at, 16), idesc | side / 8 << 17, term > 0 || k > 0);
+        }
+      }
+      ptx::commit<1>(ptx::smem(&bar));
+    }
+    __syncwarp();
+    products_done();
+    if (!ok) break;
+    if (live)
+      for (uint32_t c = (warp / 4) * 16; c < side; c += 64) {  // P = b S + c S S in S's place: every thread reads what it writes
+        float v[16];
+        tmem_load16(from + c, v);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint4* at = (uint4*)(s + small_at(side, m, c + 8 * h));
+          uint4* at_lo = (uint4*)((unsigned char*)at + s_plane);
+          float t[8], f[8];
+          unpack_half(*at, t);
+          unpack_half(*at_lo, f);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) t[k] = fmaf(p.cc, v[8 * h + k] * kPlaneUnscale, p.cb * (t[k] + f[k]));
+          uint4 hi, lo;
+          split8(t, hi, lo);
+          *at = hi;
+          *at_lo = lo;
+        }
+      }
+    written();
+    if (warp == 0 && ptx::elect()) {  // P X
+      for (uint32_t n = 0; n < length; n += 256) {
+        const uint32_t wide = min(256u, length - n);
+        for (int term = 0; term < 3; ++term) {
+          const uint32_t a = ptx::smem(s) + (term == 1 ? s_plane : 0), b = ptx::smem(x) + (term == 0 ? x_plane : 0) + n / 64 * side * 128;
+          for (uint32_t k = 0; k < side; k += 16)
+            ptx::mma<1>(tmem + n, small_descriptor(a + (k / 64) * side * 128 + (k % 64) * 2, 16), small_descriptor(b + k * 128, side * 128),
+                        idesc | 1u << 16 | wide / 8 << 17, term > 0 || k > 0);
+        }
+      }
+      ptx::commit<1>(ptx::smem(&bar));
+    }
+    __syncwarp();
+    products_done();
+    if (!ok) break;
+    if (live)
+      for (uint32_t c = (warp / 4) * 16; c < length; c += 64) {
+        float v[16];
+        tmem_load16(from + c, v);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint4* at = (uint4*)(x + small_at(side, m, c + 8 * h));
+          uint4* at_lo = (uint4*)((unsigned char*)at + x_plane);
+          float t[8], f[8];
+          unpack_half(*at, t);
+          unpack_half(*at_lo, f);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) t[k] = fmaf(p.ca, t[k] + f[k], v[8 * h + k] * kPlaneUnscale);
+          if (!last) {
+            uint4 hi, lo;
+            split8(t, hi, lo);
+            *at = hi;
+            *at_lo = lo;
+            continue;
+          }
+          // row m, columns c + 8 h ... of the iterate: a row of the matrix, or a piece of eight of its rows' column m
+          const uint32_t col = c + 8 * h;
+          if (m >= (tall ? cols : rows) || col >= (tall ? rows : cols)) continue;
+          const int count = min(8u, (tall ? rows : cols) - col);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) t[k] *= kPlaneUnscale;
+          if (!kStep) {
+            T* out = (T*)p.out + blockIdx.x * p.out_batch;
+            if (!tall) {
+              store8(out + m * p.out_row + col, count, t);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                if (k < count) out[(int64_t)(col + k) * p.out_row + m] = (T)t[k];
+            }
+            continue;
+          }
+          const int64_t first = (int64_t)p.matrix[which].offset + (tall ? (int64_t)col * cols + m : (int64_t)m * cols + col);
+          const float scale = p.matrix[which].scale;
+          const int peer = p.pull.peers[worker * p.pull.draw_stride];
+          const bool pull = peer != worker && (uint32_t)peer < (uint32_t)p.pull.workers;
+          const float weight = pull ? p.pull.weights[worker * p.pull.draw_stride] : 0.0f;
+          const T* own = (const T*)p.pull.x + worker * p.pull.x_row + first;
+          const T* other = (const T*)p.pull.x + (pull ? peer : worker) * p.pull.x_row + first;
+          T* next = (T*)p.pull.x_next + worker * p.pull.next_row + first;
+          float xi[8], xm[8];
+          if (!tall) {
+            load8(own, count, xi);
+            load8(other, count, xm);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              xi[k] = k < count ? (float)own[k * cols] : 0.0f;
+              xm[k] = k < count ? (float)other[k * cols] : 0.0f;
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float y = fmaf(-p.pull.lr, fmaf(p.pull.decay, xi[k], scale * t[k]), xi[k]);
+            t[k] = pull ? fmaf(-weight, y - xm[k], y) : y;
+          }
+          if (!tall) {
+            store8(next, count, t);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              if (k < count) next[k * cols] = (T)t[k];
+          }
+        }
+      }
+    written();
+  }
+  if (!ok && threadIdx.x == 0) {
+    *(volatile unsigned int*)p.error = 1;
+    __threadfence_system();
+  }
+  ptx::fence_before();
+  __syncthreads();
+  ptx::fence_after();
+  if (warp == 0) ptx::tmem_free<1>(tmem, p.tmem_columns);
+}
+
+}  // namespace netmax
