@@ -24,7 +24,6 @@ namespace {
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr size_t kHeader = 256;                      // of a workspace: the error word
 constexpr size_t kProductSmem = (size_t)225 * 1024;  // dynamic shared memory that a launch may take
-constexpr size_t kSlots = 8 * kSlotBytes;            // of it, the epilogue's
 constexpr size_t kLeastSmem = (size_t)120 * 1024;    // more than half an SM's: no two of these CTAs, which take all of TMEM, share one
 
 int fail_op(int code, const char* fmt, ...) {
@@ -206,12 +205,20 @@ int check_registers(const void* kernel) {
     OP_CUDA(cudaFuncGetAttributes(&a, kernel));
     registers = a.numRegs;
   }
-  if (registers * kProductThreads < (2 * 216 + 72) * 128) return fail_op(NETMAX_CUDA_ERROR, "a product kernel was built with %d registers, 168 needed", registers);
+  if (registers * product_threads(2) < (2 * 216 + 72) * 128) return fail_op(NETMAX_CUDA_ERROR, "a product kernel was built with %d registers, 168 needed", registers);
   return NETMAX_OK;
 }
 
 // Chooses the tile shape for all groups of a launch and runs it.
 int run_products(Stream& s, ProductParams& p, const int* batches, bool bf16, int epilogue) {
+  for (int k = 0; k < p.groups; ++k) {
+    ProductGroup& g = p.group[k];
+    const int64_t unit = epilogue == kLayerBf16 || epilogue == kLastBf16 ? 8 : 4;
+    auto fits = [&](const void* at, int64_t row, int64_t batch) { return ((uintptr_t)at & 15) == 0 && row % unit == 0 && (batches[k] == 1 || batch % unit == 0); };
+    const bool layer = epilogue == kLayerF32 || epilogue == kLayerBf16;
+    g.pieces = g.N % 8 == 0 && fits(g.out, g.out_row, g.out_batch) && (!layer || ((!g.z || fits(g.z, g.z_row, g.z_batch)) &&
+               (!g.residual || fits(g.residual, g.residual_row, g.residual_batch))));
+  }
   const int sms = sm_count();
   auto tiles_of = [&](const ProductGroup& g, int batch, int tile_m, int bn) {
     const int64_t tm = ceil_div(g.M, tile_m), tn = ceil_div(g.N, bn);
@@ -244,15 +251,16 @@ int run_products(Stream& s, ProductParams& p, const int* batches, bool bf16, int
   p.a_bytes = 128 * 128;
   p.b_bytes = (uint32_t)most_b * 128;
   p.stage_bytes = (uint32_t)p.planes * (p.a_bytes + p.b_bytes);
-  p.stages = (int)std::min<size_t>(kMaxStages, (kProductSmem - 1024 - kSlots) / p.stage_bytes);
-  const size_t smem = std::max(kLeastSmem, (size_t)1024 + kSlots + (size_t)p.stages * p.stage_bytes);
+  const size_t slots = (size_t)epilogue_warps(p.planes) * kSlotBytes;
+  p.stages = (int)std::min<size_t>(kMaxStages, (kProductSmem - 1024 - slots) / p.stage_bytes);
+  const size_t smem = std::max(kLeastSmem, (size_t)1024 + slots + (size_t)p.stages * p.stage_bytes);
   p.error = s.error;
   p.clear_error = s.clear;
   ProductKernel kernel = ctas == 2 ? pick_product<2>(epilogue, p.planes) : pick_product<1>(epilogue, p.planes);
   OP_CUDA(raise_smem_limit((const void*)kernel, smem));
   if (p.planes == 2) OP_DO(check_registers((const void*)kernel));
   const int grid = (int)std::min<int64_t>(tiles, sms / ctas) * ctas;
-  OP_DO(launch(s, kernel, dim3(grid), kProductThreads, smem, ctas, p));
+  OP_DO(launch(s, kernel, dim3(grid), product_threads(p.planes), smem, ctas, p));
   s.clear = false;
   return NETMAX_OK;
 }

@@ -11,8 +11,8 @@
 //
 // One CTA pair (cta_group::2) works on a tile of 256 x up to 256, each CTA with its own 128 rows of A and half the rows of B in
 // shared memory: a tile of k = 64 then costs an SM 32 KB from L2 for 512 cycles of tensor work, 48 KB if every CTA worked for
-// itself.  Problems that would leave SMs without a tile that way take one CTA per tile of 128 x 64 to 128 x 256.  Warps 0-7 are the
-// epilogue, warp 8 issues the TMA loads, warp 9 the products; the accumulators are double-buffered so that the epilogue of a tile
+// itself.  Problems that would leave SMs without a tile that way take one CTA per tile of 128 x 64 to 128 x 256.  The first warps are the
+// epilogue, one issues the TMA loads, one the products; the accumulators are double-buffered so that the epilogue of a tile
 // runs under the products of the next.
 //
 // A thread of the epilogue reads one row of 32 columns from TMEM.  Handled as they come, loads and stores of such rows touch 32 lines each
@@ -31,7 +31,10 @@
 
 namespace netmax {
 
-constexpr int kProductThreads = 384;      // eight epilogue warps, one that loads, one that multiplies, two that fill their warpgroup
+// Epilogue warps: sixteen where a thread holds one chunk, eight where it holds sums of 128 columns.  Behind them one warp loads, one
+// multiplies and two fill their warpgroup.
+__host__ __device__ constexpr int epilogue_warps(int planes) { return planes == 1 ? 16 : 8; }
+__host__ __device__ constexpr int product_threads(int planes) { return (epilogue_warps(planes) + 4) * 32; }
 constexpr int kSlotBytes = 4096;          // of an epilogue warp: 32 x 32 fp32
 constexpr int kProductBox = 64;           // a TMA box: 64 rows of 64 16-bit values (128 bytes, the swizzle's width)
 constexpr int kBoxBytes = kProductBox * 128;
@@ -72,6 +75,7 @@ struct ProductGroup {
   int32_t activation = 0;
   const int32_t *exp_a = nullptr, *exp_b = nullptr;  // per matrix: its planes hold 2^exp times the values
   int32_t first_matrix = 0;                          // of the step's table
+  int32_t pieces = 0;                                // every row of every view above starts on a 16-byte boundary, and N is a multiple of 8
 };
 
 struct PullParams {  // a worker's local step and pull, behind the last product
@@ -264,10 +268,10 @@ __device__ __forceinline__ Tile find_tile(const ProductParams& p, int t) {
   return r;
 }
 
-// Eight values of a type, in 16-byte pieces where the address allows it; `count` of them exist.
-template <typename T>
+// Eight values of a type, in 16-byte pieces where the address allows it (kWhole: it does); `count` of them exist.
+template <typename T, bool kWhole = false>
 __device__ __forceinline__ void load8(const T* at, int count, float (&v)[8]) {
-  if (count == 8 && ((uintptr_t)at & 15) == 0) {
+  if (kWhole || (count == 8 && ((uintptr_t)at & 15) == 0)) {
     if (sizeof(T) == 4) {
       const float4 a = ((const float4*)at)[0], b = ((const float4*)at)[1];
       v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
@@ -280,29 +284,29 @@ __device__ __forceinline__ void load8(const T* at, int count, float (&v)[8]) {
         v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
       }
     }
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) v[k] = k < count ? (float)at[k] : 0.0f;
+    for (int k = 0; k < 8; ++k) v[k] = k < count ? (float)at[k] : 0.0f;
+  }
 }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *(const uint32_t*)&h;
 }
-template <typename T>
+template <typename T, bool kWhole = false>
 __device__ __forceinline__ void store8(T* at, int count, const float (&v)[8]) {
-  if (count == 8 && ((uintptr_t)at & 15) == 0) {
+  if (kWhole || (count == 8 && ((uintptr_t)at & 15) == 0)) {
     if (sizeof(T) == 4) {
       ((float4*)at)[0] = make_float4(v[0], v[1], v[2], v[3]);
       ((float4*)at)[1] = make_float4(v[4], v[5], v[6], v[7]);
     } else {
       *(uint4*)at = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
     }
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
-    if (k < count) at[k] = (T)v[k];
+    for (int k = 0; k < 8; ++k)
+      if (k < count) at[k] = (T)v[k];
+  }
 }
 __device__ __forceinline__ void unpack_half(const uint4& a, float (&v)[8]) {
   const uint32_t w[4] = {a.x, a.y, a.z, a.w};
@@ -312,6 +316,15 @@ __device__ __forceinline__ void unpack_half(const uint4& a, float (&v)[8]) {
     v[2 * k] = f.x;
     v[2 * k + 1] = f.y;
   }
+}
+__device__ __forceinline__ uint4 half8(const float (&v)[8]) {
+  uint32_t h[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const __half2 a = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+    h[k] = *(const uint32_t*)&a;
+  }
+  return make_uint4(h[0], h[1], h[2], h[3]);
 }
 // Eight values as two planes.
 __device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {
@@ -335,15 +348,15 @@ struct Residual {
 template <int kEpilogue, int kPlanes>
 __device__ __forceinline__ void load_residual(const ProductGroup& g, int q, int m0, int n0, int lane, Residual& r) {
   if (kEpilogue < kPolynomial) return;
-  const int n = n0 + 8 * (lane % 4);
-  const __half* at = (const __half*)g.residual + q * g.residual_batch + n;
+  const int n = n0 + 8 * (lane % 4), row = lane / 4, rows = n < g.N ? g.M - m0 - row : 0;  // (planes' rows are padded to eight columns)
+  const __half* at = (const __half*)g.residual + q * g.residual_batch + (int64_t)(m0 + row) * g.residual_row + n;
+  const int64_t step = 8 * g.residual_row;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int m = m0 + 8 * i + lane / 4;
+  for (int i = 0; i < 4; ++i, at += step) {
     r.hi[i] = r.lo[i] = make_uint4(0, 0, 0, 0);
-    if (m < g.M && n < g.N) {  // (planes' rows are padded to eight columns)
-      r.hi[i] = *(const uint4*)(at + (int64_t)m * g.residual_row);
-      if (kEpilogue > kPolynomial || kPlanes == 2) r.lo[i] = *(const uint4*)(at + (int64_t)m * g.residual_row + g.residual_plane);
+    if (8 * i < rows) {
+      r.hi[i] = *(const uint4*)at;
+      if (kEpilogue > kPolynomial || kPlanes == 2) r.lo[i] = *(const uint4*)(at + g.residual_plane);
     }
   }
 }
@@ -357,6 +370,103 @@ __device__ __forceinline__ void stage_row(float* slot, const float (&acc)[32]) {
     *(float4*)(slot + lane * 32 + (c ^ (lane & 7)) * 4) = make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
 }
 
+__device__ __forceinline__ void activate8(float (&v)[8], int activation) {
+  if (activation == kActRelu) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = activate(v[k], kActRelu);
+  } else if (activation == kActGelu) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = activate(v[k], kActGelu);
+  } else if (activation == kActSilu) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = activate(v[k], kActSilu);
+  }
+}
+// A lane's eight columns of row `row` of the staged chunk.
+__device__ __forceinline__ void read_slot(const float* slot, int row, int c, float (&v)[8]) {
+  const float4 a = *(const float4*)(slot + row * 32 + ((2 * c) ^ (row & 7)) * 4), b = *(const float4*)(slot + row * 32 + ((2 * c + 1) ^ (row & 7)) * 4);
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+
+// y and z of a chunk.  kWhole: all 32 x 32 elements exist, in 16-byte pieces.
+template <typename T, bool kWhole>
+__device__ __forceinline__ void layer_chunk(const ProductGroup& g, int q, int m0, int n0, int exponent, const float* slot) {
+  const int lane = threadIdx.x % 32, c = lane % 4, n = n0 + 8 * c, row = lane / 4, count = kWhole ? 8 : min(8, g.N - n), rows = kWhole ? 32 : g.M - m0 - row;
+  float bias[8];
+  if (g.bias) {
+    const T* b = (const T*)g.bias + q * g.bias_batch + n;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) bias[k] = kWhole || k < count ? (float)b[k] : 0.0f;
+  }
+  // 2^exponent as two factors, so that neither leaves fp32's range
+  const float f0 = ldexpf(1.0f, exponent / 2), f1 = ldexpf(1.0f, exponent - exponent / 2);
+  const T* r = (const T*)g.residual + q * g.residual_batch + (int64_t)(m0 + row) * g.residual_row + n;
+  T* z = (T*)g.z + q * g.z_batch + (int64_t)(m0 + row) * g.z_row + n;
+  T* y = (T*)g.out + q * g.out_batch + (int64_t)(m0 + row) * g.out_row + n;
+#pragma unroll kWhole ? 4 : 1
+  for (int i = 0; i < 4; ++i, r += 8 * g.residual_row, z += 8 * g.z_row, y += 8 * g.out_row) {
+    if (!kWhole && (8 * i >= rows || count <= 0)) break;
+    float v[8], add[8];
+    if (g.residual) load8<T, kWhole>(r, count, add);
+    read_slot(slot, 8 * i + row, c, v);
+    if (sizeof(T) == 4) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = v[k] * f0 * f1;
+    }
+    if (g.bias) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += bias[k];
+    }
+    if (g.z) store8<T, kWhole>(z, count, v);
+    activate8(v, g.activation);
+    if (g.residual) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += add[k];
+    }
+    store8<T, kWhole>(y, count, v);
+  }
+}
+
+// The local step and the pull of a chunk of a worker's matrix.
+template <typename T>
+__device__ __forceinline__ void step_chunk(const ProductParams& p, const ProductGroup& g, int q, int m0, int n0, const float* slot, const Residual& residual) {
+  const int lane = threadIdx.x % 32, c = lane % 4, n = n0 + 8 * c, row = lane / 4, count = min(8, g.N - n), rows = count > 0 ? g.M - m0 - row : 0;
+  const PullParams& s = p.step;
+  const int matrix = g.first_matrix + q / s.workers, worker = q % s.workers;
+  const float scale = p.matrix_scale[matrix] * kPlaneUnscale;
+  const int peer = s.peers[worker * s.draw_stride];
+  const bool pull = peer != worker && (uint32_t)peer < (uint32_t)s.workers;
+  const float w = pull ? s.weights[worker * s.draw_stride] : 0.0f;
+  const int64_t at = (int64_t)p.matrix_offset[matrix] + (int64_t)(m0 + row) * g.out_row + n, step = 8 * g.out_row;
+  const T* own = (const T*)s.x + worker * s.x_row + at;
+  const T* other = (const T*)s.x + (pull ? peer : worker) * s.x_row + at;
+  T* next = (T*)s.x_next + worker * s.next_row + at;
+  const bool whole = count == 8 && (((uintptr_t)own | (uintptr_t)other | (uintptr_t)next | (uintptr_t)(step * sizeof(T))) & 15) == 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i, own += step, other += step, next += step) {
+    if (8 * i >= rows) break;
+    float xi[8], xm[8], v[8], x[8], lo[8];
+    if (whole) {
+      load8<T, true>(own, 8, xi);
+      load8<T, true>(other, 8, xm);
+    } else {
+      load8<T, false>(own, count, xi);
+      load8<T, false>(other, count, xm);
+    }
+    read_slot(slot, 8 * i + row, c, v);
+    unpack_half(residual.hi[i], x);
+    unpack_half(residual.lo[i], lo);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float o = scale * fmaf(p.ca, x[k] + lo[k], v[k] * kPlaneUnscale);
+      const float h = fmaf(-s.lr, fmaf(s.decay, xi[k], o), xi[k]);
+      v[k] = pull ? fmaf(-w, h - xm[k], h) : h;
+    }
+    if (whole) store8<T, true>(next, 8, v);
+    else store8<T, false>(next, count, v);
+  }
+}
+
 // Rows m0 ... m0 + 31 and columns n0 ... n0 + 31 of the accumulator, which the warp has staged.  Called from one place in a loop: unrolled
 // over a tile's chunks the code outgrew the instruction cache (the 8 x (4096 x 4096 x 4096) layer with silu: 1715 us).
 template <int kEpilogue, int kPlanes>
@@ -364,120 +474,83 @@ __device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const Pro
                                                const Residual& residual) {
   const int lane = threadIdx.x % 32;
   __syncwarp();
-  const int c = lane % 4, n = n0 + 8 * c, count = min(8, g.N - n);
-  const bool mirrored = (kEpilogue == kGram || kEpilogue == kPolynomial) && t.i != t.j;
-  float bias[8];
   if (kEpilogue == kLayerF32 || kEpilogue == kLayerBf16) {
     using T = typename std::conditional<kEpilogue == kLayerF32, float, __nv_bfloat16>::type;
-    const T* b = g.bias && count > 0 ? (const T*)g.bias + t.q * g.bias_batch + n : nullptr;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) bias[k] = b && k < count ? (float)b[k] : 0.0f;
+    if (g.pieces && m0 + 32 <= g.M && n0 + 32 <= g.N) layer_chunk<T, true>(g, t.q, m0, n0, exponent, slot);
+    else layer_chunk<T, false>(g, t.q, m0, n0, exponent, slot);
+    return;
   }
+  if (kEpilogue == kStepF32 || kEpilogue == kStepBf16) {
+    using T = typename std::conditional<kEpilogue == kStepF32, float, __nv_bfloat16>::type;
+    step_chunk<T>(p, g, t.q, m0, n0, slot, residual);
+    return;
+  }
+  const int c = lane % 4, n = n0 + 8 * c, row = lane / 4, count = min(8, g.N - n), rows = count > 0 ? g.M - m0 - row : 0;
+  if (kEpilogue == kLastF32 || kEpilogue == kLastBf16) {
+    using T = typename std::conditional<kEpilogue == kLastF32, float, __nv_bfloat16>::type;
+    T* out = (T*)g.out + t.q * g.out_batch + (int64_t)(m0 + row) * g.out_row + n;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = 8 * i + lane / 4, m = m0 + row;
-    float4* at0 = (float4*)(slot + row * 32 + ((2 * c) ^ (row & 7)) * 4);
-    float4* at1 = (float4*)(slot + row * 32 + ((2 * c + 1) ^ (row & 7)) * 4);
-    const float4 a0 = *at0, a1 = *at1;
-    float v[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
-    if (m >= g.M || count <= 0) continue;
-    if (kEpilogue == kLayerF32 || kEpilogue == kLayerBf16) {
-      using T = typename std::conditional<kEpilogue == kLayerF32, float, __nv_bfloat16>::type;
-      if (kEpilogue == kLayerF32) {
-        const float f0 = ldexpf(1.0f, exponent / 2), f1 = ldexpf(1.0f, exponent - exponent / 2);  // (in two factors: neither overflows)
+    for (int i = 0; i < 4; ++i, out += 8 * g.out_row) {
+      if (8 * i >= rows) break;
+      float v[8], x[8], lo[8];
+      read_slot(slot, 8 * i + row, c, v);
+      unpack_half(residual.hi[i], x);
+      unpack_half(residual.lo[i], lo);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = v[k] * f0 * f1;
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] += bias[k];
-      float add[8];
-      if (g.residual) load8((const T*)g.residual + t.q * g.residual_batch + m * g.residual_row + n, count, add);
-      if (g.z) store8((T*)g.z + t.q * g.z_batch + m * g.z_row + n, count, v);
-      if (g.activation == kActRelu) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = activate(v[k], kActRelu);
-      } else if (g.activation == kActGelu) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = activate(v[k], kActGelu);
-      } else if (g.activation == kActSilu) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = activate(v[k], kActSilu);
-      }
-      if (g.residual) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] += add[k];
-      }
-      store8((T*)g.out + t.q * g.out_batch + m * g.out_row + n, count, v);
-      continue;
+      for (int k = 0; k < 8; ++k) v[k] = kPlaneUnscale * fmaf(p.ca, x[k] + lo[k], v[k] * kPlaneUnscale);
+      if (g.pieces) store8<T, true>(out, 8, v);
+      else store8<T, false>(out, count, v);
     }
-    float hi[8], lo[8];
+    return;
+  }
+  const bool mirrored = kEpilogue != kUpdate && t.i != t.j;
+  __half* out = (__half*)g.out + t.q * g.out_batch + (int64_t)(m0 + row) * g.out_row + n;
+#pragma unroll
+  for (int i = 0; i < 4; ++i, out += 8 * g.out_row) {
+    if (8 * i >= rows) break;
+    float v[8], x[8], lo[8];
+    read_slot(slot, 8 * i + row, c, v);
     if (kEpilogue >= kPolynomial) {
-      unpack_half(residual.hi[i], hi);
-      if (kEpilogue > kPolynomial || kPlanes == 2) {
+      unpack_half(residual.hi[i], x);
+      if (kEpilogue == kUpdate || kPlanes == 2) {
         unpack_half(residual.lo[i], lo);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) hi[k] += lo[k];
+        for (int k = 0; k < 8; ++k) x[k] += lo[k];
       }
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       v[k] *= kPlaneUnscale;
-      if (kEpilogue == kPolynomial) v[k] = fmaf(p.cc, v[k], p.cb * hi[k]);
-      if (kEpilogue > kPolynomial) v[k] = fmaf(p.ca, hi[k], v[k]);
+      if (kEpilogue == kPolynomial) v[k] = fmaf(p.cc, v[k], p.cb * x[k]);
+      if (kEpilogue == kUpdate) v[k] = fmaf(p.ca, x[k], v[k]);
     }
-    if (kEpilogue == kGram || kEpilogue == kPolynomial || kEpilogue == kUpdate) {
-      uint4 h, l;
-      split8(v, h, l);
-      __half* out = (__half*)g.out + t.q * g.out_batch + m * g.out_row + n;
-      *(uint4*)out = h;
-      if (kEpilogue == kUpdate || kPlanes == 2) *(uint4*)(out + g.out_plane) = l;
-      if (mirrored) {  // both planes of an element in one word
-        *at0 = make_float4(__uint_as_float(__byte_perm(h.x, l.x, 0x5410)), __uint_as_float(__byte_perm(h.x, l.x, 0x7632)),
-                           __uint_as_float(__byte_perm(h.y, l.y, 0x5410)), __uint_as_float(__byte_perm(h.y, l.y, 0x7632)));
-        *at1 = make_float4(__uint_as_float(__byte_perm(h.z, l.z, 0x5410)), __uint_as_float(__byte_perm(h.z, l.z, 0x7632)),
-                           __uint_as_float(__byte_perm(h.w, l.w, 0x5410)), __uint_as_float(__byte_perm(h.w, l.w, 0x7632)));
-      }
-      continue;
+    uint4 h, l;
+    if (kEpilogue == kUpdate || kPlanes == 2) split8(v, h, l);
+    else h = half8(v), l = make_uint4(0, 0, 0, 0);
+    *(uint4*)out = h;
+    if (kEpilogue == kUpdate || kPlanes == 2) *(uint4*)(out + g.out_plane) = l;
+    if (mirrored) {  // both planes of an element in one word
+      const int r = 8 * i + row;
+      *(uint4*)(slot + r * 32 + ((2 * c) ^ (r & 7)) * 4) =
+          make_uint4(__byte_perm(h.x, l.x, 0x5410), __byte_perm(h.x, l.x, 0x7632), __byte_perm(h.y, l.y, 0x5410), __byte_perm(h.y, l.y, 0x7632));
+      *(uint4*)(slot + r * 32 + ((2 * c + 1) ^ (r & 7)) * 4) =
+          make_uint4(__byte_perm(h.z, l.z, 0x5410), __byte_perm(h.z, l.z, 0x7632), __byte_perm(h.w, l.w, 0x5410), __byte_perm(h.w, l.w, 0x7632));
     }
-    if (kEpilogue == kLastF32 || kEpilogue == kLastBf16) {
-      using T = typename std::conditional<kEpilogue == kLastF32, float, __nv_bfloat16>::type;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] *= kPlaneUnscale;
-      store8((T*)g.out + t.q * g.out_batch + m * g.out_row + n, count, v);
-      continue;
-    }
-    using T = typename std::conditional<kEpilogue == kStepF32, float, __nv_bfloat16>::type;
-    const PullParams& s = p.step;
-    const int matrix = g.first_matrix + t.q / s.workers, worker = t.q % s.workers;
-    const int64_t at = (int64_t)p.matrix_offset[matrix] + m * g.out_row + n;
-    const float scale = p.matrix_scale[matrix] * kPlaneUnscale;
-    const int peer = s.peers[worker * s.draw_stride];
-    const bool pull = peer != worker && (uint32_t)peer < (uint32_t)s.workers;
-    const float w = pull ? s.weights[worker * s.draw_stride] : 0.0f;
-    float xi[8], xm[8];
-    load8((const T*)s.x + worker * s.x_row + at, count, xi);
-    load8((const T*)s.x + (pull ? peer : worker) * s.x_row + at, count, xm);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float h = fmaf(-s.lr, fmaf(s.decay, xi[k], scale * v[k]), xi[k]);
-      v[k] = pull ? fmaf(-w, h - xm[k], h) : h;
-    }
-    store8((T*)s.x_next + worker * s.next_row + at, count, v);
   }
-  if (mirrored) {  // rows n0 + ..., columns m0 + ...
-    __syncwarp();
+  if (!mirrored) return;
+  __syncwarp();  // rows n0 + ..., columns m0 + ...
+  const int m = m0 + 8 * c;
+  out = (__half*)g.out + t.q * g.out_batch + (int64_t)(n0 + row) * g.out_row + m;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int column = 8 * i + lane / 4, m = m0 + 8 * c;
-      uint32_t w[8];
+  for (int i = 0; i < 4; ++i, out += 8 * g.out_row) {
+    const int column = 8 * i + row;
+    uint32_t w[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(slot[(8 * c + k) * 32 + ((column / 4) ^ k) * 4 + column % 4]);
-      if (n0 + column >= g.N || m >= g.M) continue;
-      __half* out = (__half*)g.out + t.q * g.out_batch + (int64_t)(n0 + column) * g.out_row + m;
-      *(uint4*)out = make_uint4(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[4], w[5], 0x5410), __byte_perm(w[6], w[7], 0x5410));
-      if (kPlanes == 2)
-        *(uint4*)(out + g.out_plane) = make_uint4(__byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632), __byte_perm(w[4], w[5], 0x7632), __byte_perm(w[6], w[7], 0x7632));
-    }
+    for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(slot[(8 * c + k) * 32 + ((column / 4) ^ k) * 4 + column % 4]);
+    if (n0 + column >= g.N || m >= g.M) continue;
+    *(uint4*)out = make_uint4(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[4], w[5], 0x5410), __byte_perm(w[6], w[7], 0x5410));
+    if (kPlanes == 2)
+      *(uint4*)(out + g.out_plane) = make_uint4(__byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632), __byte_perm(w[4], w[5], 0x7632), __byte_perm(w[6], w[7], 0x7632));
   }
 }
 
@@ -487,7 +560,8 @@ __device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const Pro
 constexpr int kPromote = 2;
 
 template <int kCtas, int kEpilogue, int kPlanes>
-__global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __grid_constant__ ProductParams p) {
+__global__ __launch_bounds__(product_threads(kPlanes), 1) void product_kernel(const __grid_constant__ ProductParams p) {
+  constexpr int kEpilogueWarps = epilogue_warps(kPlanes), kLoader = kEpilogueWarps, kMultiplier = kEpilogueWarps + 1;
   extern __shared__ unsigned char raw[];
   __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 4];
   __shared__ uint32_t tmem_at;
@@ -505,12 +579,12 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
     }
     for (int b = 0; b < 2; ++b) {
       ptx::barrier_init(done + 8 * b, 1);
-      ptx::barrier_init(drained + 8 * b, 8 * kCtas);
+      ptx::barrier_init(drained + 8 * b, kEpilogueWarps * kCtas);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     gave_up = 0;
   }
-  if (warp == 9) ptx::tmem_alloc<kCtas>(ptx::smem(&tmem_at), 512);
+  if (warp == kMultiplier) ptx::tmem_alloc<kCtas>(ptx::smem(&tmem_at), 512);
   ptx::fence_before();
   __syncthreads();
   if (kCtas == 2) ptx::cluster_sync();
@@ -527,9 +601,9 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
     __threadfence_system();
   };
   // Two planes: 128 of an epilogue thread's registers are sums.  168 a thread at the launch, 64,512 in all: (2 x 216 + 72) x 128.
-  if (warp >= 8) {
+  if (warp >= kEpilogueWarps) {
   if (kPlanes == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-  if (warp == 8 && ptx::elect()) {  // ---- loads
+  if (warp == kLoader && ptx::elect()) {  // ---- loads
     int issued = 0;  // stages filled so far
     bool ok = true;
     for (int t = first; t < p.tiles && ok; t += stride) {
@@ -566,7 +640,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
         failed();
       }
     }
-  } else if (warp == 9 && rank == 0 && ptx::elect()) {  // ---- products
+  } else if (warp == kMultiplier && rank == 0 && ptx::elect()) {  // ---- products
     int used = 0, part = 0;  // stages and accumulators so far
     bool ok = true;
     for (int t = first; t < p.tiles && ok; t += stride) {
@@ -598,7 +672,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
     }
     if (!ok) failed();
   }
-  } else {  // ---- epilogue: warp w has lanes 32 (w % 4) ... of the accumulator and every other 32 columns
+  } else {  // ---- epilogue: warp w has lanes 32 (w % 4) ... of the accumulator and every second (fourth) 32 columns from w / 4 on
     if (kPlanes == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const uint32_t quadrant = warp % 4, half = warp / 4;
     float* const slot = slots + warp * (kSlotBytes / 4);
@@ -643,14 +717,12 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
           }
         } else {
 #pragma unroll 1
-          for (int c = (int)half * 32; c < columns; c += 64) {
-            Residual next;  // of the next 32 columns, under this one's arithmetic
-            if (c + 64 < columns) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + c + 64, lane, next);
+          for (int c = (int)half * 32; c < columns; c += 8 * kEpilogueWarps) {
+            if (c != (int)half * 32) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + c, lane, residual);
             ptx::tmem_load32(from + c, sum[0]);
             __syncwarp();
             stage_row(slot, sum[0]);
             epilogue_chunk<kEpilogue, kPlanes>(p, g, tile, m0, n0 + c, exponent, slot, residual);
-            residual = next;
           }
         }
         ptx::fence_before();
@@ -681,7 +753,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
   __syncthreads();
   if (kCtas == 2) ptx::cluster_sync();  // (neither CTA's shared memory goes while the other may still signal it)
   ptx::fence_after();
-  if (warp == 9) ptx::tmem_free<kCtas>(tmem, 512);
+  if (warp == kMultiplier) ptx::tmem_free<kCtas>(tmem, 512);
 }
 
 }  // namespace netmax
