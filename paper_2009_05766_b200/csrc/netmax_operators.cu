@@ -133,19 +133,27 @@ struct Operand {
   bool bf16 = false;
   int64_t inner = 0, outer = 0, row = 0, batch = 0, plane = 0;
   int count = 1, planes = 1;
+  // maps for boxes of 64 and 128 rows, made when a launch first asks for them
+  mutable bool have[2] = {false, false};
+  mutable CUtensorMap map[2];
 };
-int encode(const Operand& o, CUtensorMap* map) {
-  const EncodeTiled f = encoder();
-  if (!f) return fail_op(NETMAX_CUDA_ERROR, "the driver has no cuTensorMapEncodeTiled");
-  const cuuint64_t dims[4] = {(cuuint64_t)o.inner, (cuuint64_t)o.outer, (cuuint64_t)o.count, (cuuint64_t)o.planes};
-  const int64_t whole = o.row * std::max<int64_t>(1, o.outer);
-  const cuuint64_t strides[3] = {(cuuint64_t)o.row * 2, (cuuint64_t)(o.count > 1 ? o.batch : whole) * 2, (cuuint64_t)(o.planes > 1 ? o.plane : whole) * 2};
-  const cuuint32_t box[4] = {kProductBox, kProductBox, 1, 1}, steps[4] = {1, 1, 1, 1};
-  const CUresult r = f(map, o.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(o.data), dims, strides, box, steps,
-                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS)
-    return fail_op(NETMAX_CUDA_ERROR, "cuTensorMapEncodeTiled: error %d (%lld x %lld, row %lld, %d matrices %lld apart)", (int)r, (long long)o.outer,
-                   (long long)o.inner, (long long)o.row, o.count, (long long)o.batch);
+int tensor_map(const Operand& o, int box_rows, CUtensorMap* out) {
+  const int k = box_rows == 128;
+  if (!o.have[k]) {
+    const EncodeTiled f = encoder();
+    if (!f) return fail_op(NETMAX_CUDA_ERROR, "the driver has no cuTensorMapEncodeTiled");
+    const cuuint64_t dims[4] = {(cuuint64_t)o.inner, (cuuint64_t)o.outer, (cuuint64_t)o.count, (cuuint64_t)o.planes};
+    const int64_t whole = o.row * std::max<int64_t>(1, o.outer);
+    const cuuint64_t strides[3] = {(cuuint64_t)o.row * 2, (cuuint64_t)(o.count > 1 ? o.batch : whole) * 2, (cuuint64_t)(o.planes > 1 ? o.plane : whole) * 2};
+    const cuuint32_t box[4] = {kProductBox, (cuuint32_t)box_rows, 1, 1}, steps[4] = {1, 1, 1, 1};
+    const CUresult r = f(&o.map[k], o.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(o.data), dims, strides, box,
+                         steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS)
+      return fail_op(NETMAX_CUDA_ERROR, "cuTensorMapEncodeTiled: error %d (%lld x %lld, row %lld, %d matrices %lld apart)", (int)r, (long long)o.outer,
+                     (long long)o.inner, (long long)o.row, o.count, (long long)o.batch);
+    o.have[k] = true;
+  }
+  *out = o.map[k];
   return NETMAX_OK;
 }
 
@@ -209,12 +217,18 @@ int check_registers(const void* kernel) {
   return NETMAX_OK;
 }
 
+// What a group of a launch multiplies.
+struct Factors {
+  const Operand *a = nullptr, *b = nullptr;
+  int batch = 0;
+};
+
 // Chooses the tile shape for all groups of a launch and runs it.
-int run_products(Stream& s, ProductParams& p, const int* batches, bool bf16, int epilogue) {
+int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilogue) {
   for (int k = 0; k < p.groups; ++k) {
     ProductGroup& g = p.group[k];
     const int64_t unit = epilogue == kLayerBf16 || epilogue == kLastBf16 ? 8 : 4;
-    auto fits = [&](const void* at, int64_t row, int64_t batch) { return ((uintptr_t)at & 15) == 0 && row % unit == 0 && (batches[k] == 1 || batch % unit == 0); };
+    auto fits = [&](const void* at, int64_t row, int64_t batch) { return ((uintptr_t)at & 15) == 0 && row % unit == 0 && (factors[k].batch == 1 || batch % unit == 0); };
     const bool layer = epilogue == kLayerF32 || epilogue == kLayerBf16;
     g.pieces = g.N % 8 == 0 && fits(g.out, g.out_row, g.out_batch) && (!layer || ((!g.z || fits(g.z, g.z_row, g.z_batch)) &&
                (!g.residual || fits(g.residual, g.residual_row, g.residual_batch))));
@@ -227,8 +241,8 @@ int run_products(Stream& s, ProductParams& p, const int* batches, bool bf16, int
   int64_t pairs = 0, wide = 0;
   for (int k = 0; k < p.groups; ++k) {
     const ProductGroup& g = p.group[k];
-    pairs += tiles_of(g, batches[k], 256, g.symmetric || g.N > 128 ? 256 : 128);
-    wide += tiles_of(g, batches[k], 128, 128);
+    pairs += tiles_of(g, factors[k].batch, 256, g.symmetric || g.N > 128 ? 256 : 128);
+    wide += tiles_of(g, factors[k].batch, 128, 128);
   }
   const int ctas = pairs * 5 >= sms / 2 * 4 ? 2 : 1;
   int64_t tiles = 0;
@@ -240,8 +254,13 @@ int run_products(Stream& s, ProductParams& p, const int* batches, bool bf16, int
     g.tiles_m = ceil_div(g.M, 128 * ctas);
     g.tiles_n = ceil_div(g.N, g.bn);
     g.tile_begin = (int)tiles;
-    tiles += tiles_of(g, batches[k], 128 * ctas, g.bn);
-    g.idesc = 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (uint32_t)g.a_mn << 15 | (uint32_t)g.b_mn << 16 | (uint32_t)(g.bn / 8) << 17 |
+    tiles += tiles_of(g, factors[k].batch, 128 * ctas, g.bn);
+    // the longer a box, the fewer of them: 128 rows of a k-contiguous operand (8 x 4096^3: 950 us with boxes of 64, 880 so)
+    g.a_box = g.a_mn ? 64 : 128;
+    g.b_box = g.b_mn || g.bn / ctas < 128 ? 64 : 128;
+    OP_DO(tensor_map(*factors[k].a, g.a_box, &g.a));
+    OP_DO(tensor_map(*factors[k].b, g.b_box, &g.b));
+    g.idesc = 1u << 4 | (factors[k].a->bf16 ? 1u << 7 | 1u << 10 : 0u) | (uint32_t)g.a_mn << 15 | (uint32_t)g.b_mn << 16 | (uint32_t)(g.bn / 8) << 17 |
               (uint32_t)(128 * ctas / 16) << 24;
     most_b = std::max(most_b, g.bn / ctas);
   }
@@ -539,8 +558,6 @@ int netmax_layer_forward(const netmax_layer* l) try {
   p.planes = l->storage == NETMAX_STORAGE_F32 ? 2 : 1;
   ProductGroup& g = p.group[0];
   fill_product(g, x, false, w, false, n, n_out, n_in);
-  OP_DO(encode(x.operand, &g.a));
-  OP_DO(encode(w.operand, &g.b));
   g.out = l->y.data;
   g.out_row = l->y.row_stride;
   g.out_batch = l->y.worker_stride;
@@ -553,8 +570,8 @@ int netmax_layer_forward(const netmax_layer* l) try {
   g.residual_row = l->residual.row_stride;
   g.residual_batch = l->residual.worker_stride;
   g.activation = l->activation;
-  const int batch = l->M;
-  return run_products(s, p, &batch, w.operand.bf16, w.operand.bf16 ? kLayerBf16 : kLayerF32);
+  const Factors factors{&x.operand, &w.operand, l->M};
+  return run_products(s, p, &factors, w.operand.bf16 ? kLayerBf16 : kLayerF32);
 } NM_CATCH(fail_caught)
 
 int netmax_layer_backward(const netmax_layer* l) try {
@@ -633,28 +650,24 @@ int netmax_layer_backward(const netmax_layer* l) try {
   }
   ProductParams p;
   p.planes = f32 ? 2 : 1;
-  int batches[2];
+  Factors factors[2];
   if (l->dx.data) {
     ProductGroup& g = p.group[p.groups];
-    batches[p.groups++] = l->M;
+    factors[p.groups++] = {&dz.operand, &w.operand, l->M};
     fill_product(g, dz, false, w, true, n, n_in, n_out);
-    OP_DO(encode(dz.operand, &g.a));
-    OP_DO(encode(w.operand, &g.b));
     g.out = l->dx.data;
     g.out_row = l->dx.row_stride;
     g.out_batch = l->dx.worker_stride;
   }
   if (l->dweight.data) {
     ProductGroup& g = p.group[p.groups];
-    batches[p.groups++] = l->M;
+    factors[p.groups++] = {&dz.operand, &x.operand, l->M};
     fill_product(g, dz, true, x, true, n_out, n_in, n);
-    OP_DO(encode(dz.operand, &g.a));
-    OP_DO(encode(x.operand, &g.b));
     g.out = l->dweight.data;
     g.out_row = l->dweight.row_stride;
     g.out_batch = l->dweight.worker_stride;
   }
-  return run_products(s, p, batches, !f32, f32 ? kLayerF32 : kLayerBf16);
+  return run_products(s, p, factors, f32 ? kLayerF32 : kLayerBf16);
 } NM_CATCH(fail_caught)
 
 }  // extern "C"
@@ -671,7 +684,7 @@ struct SchulzGroup {
   int64_t side = 0;
   __half *x[2] = {nullptr, nullptr}, *gram = nullptr, *poly = nullptr;
   int64_t x_row = 0, x_batch = 0, x_plane = 0, s_row = 0, s_batch = 0, s_plane = 0;
-  CUtensorMap map_x[2], map_gram, map_poly;
+  Operand op_x[2], op_gram, op_poly;
   void set(int64_t r, int64_t c, int n) {
     rows = r;
     cols = c;
@@ -690,28 +703,27 @@ struct SchulzGroup {
     gram = (__half*)carver.take((size_t)s_plane * (size_t)planes * sizeof(__half));
     poly = (__half*)carver.take((size_t)s_plane * (size_t)planes * sizeof(__half));
   }
-  int encode_maps(int planes) {
-    Operand o;
-    o.inner = cols;
-    o.outer = rows;
-    o.row = x_row;
-    o.batch = x_batch;
-    o.plane = x_plane;
-    o.count = batch;
-    o.planes = 2;
+  void describe(int planes) {  // (behind take())
     for (int k = 0; k < 2; ++k) {
+      Operand& o = op_x[k];
       o.data = x[k];
-      OP_DO(encode(o, &map_x[k]));
+      o.inner = cols;
+      o.outer = rows;
+      o.row = x_row;
+      o.batch = x_batch;
+      o.plane = x_plane;
+      o.count = batch;
+      o.planes = 2;
     }
-    o.inner = o.outer = side;
-    o.row = s_row;
-    o.batch = s_batch;
-    o.plane = s_plane;
-    o.planes = planes;
-    o.data = gram;
-    OP_DO(encode(o, &map_gram));
-    o.data = poly;
-    return encode(o, &map_poly);
+    for (Operand* o : {&op_gram, &op_poly}) {
+      o->data = o == &op_gram ? gram : poly;
+      o->inner = o->outer = side;
+      o->row = s_row;
+      o->batch = s_batch;
+      o->plane = s_plane;
+      o->count = batch;
+      o->planes = planes;
+    }
   }
 };
 
@@ -730,18 +742,18 @@ int run_schulz(Stream& s, std::vector<SchulzGroup>& groups, int steps, int plane
       const bool final = phase == 2 && step + 1 == steps;
       for (size_t first = 0; first < groups.size(); first += kMaxGroups) {
         const size_t n = std::min<size_t>(kMaxGroups, groups.size() - first);
-        int batches[kMaxGroups];
+        Factors factors[kMaxGroups];
         p.groups = (int)n;
         for (size_t k = 0; k < n; ++k) {
           const SchulzGroup& q = groups[first + k];
           ProductGroup g;
-          batches[k] = q.batch;
+          factors[k].batch = q.batch;
           if (phase < 2) {
             g.symmetric = 1;
             g.M = g.N = (int32_t)q.side;
             g.K = (int32_t)(phase == 0 && !q.tall ? q.cols : phase == 0 ? q.rows : q.side);
             g.a_mn = g.b_mn = phase == 0 && q.tall;
-            g.a = g.b = phase == 0 ? q.map_x[now] : q.map_gram;
+            factors[k].a = factors[k].b = phase == 0 ? &q.op_x[now] : &q.op_gram;
             g.out = phase == 0 ? q.gram : q.poly;
             g.out_row = q.s_row;
             g.out_batch = q.s_batch;
@@ -756,8 +768,8 @@ int run_schulz(Stream& s, std::vector<SchulzGroup>& groups, int steps, int plane
             g.M = (int32_t)q.rows;
             g.N = (int32_t)q.cols;
             g.K = (int32_t)q.side;
-            g.a = q.tall ? q.map_x[now] : q.map_poly;
-            g.b = q.tall ? q.map_poly : q.map_x[now];
+            factors[k].a = q.tall ? &q.op_x[now] : &q.op_poly;
+            factors[k].b = q.tall ? &q.op_poly : &q.op_x[now];
             g.b_mn = !q.tall;
             g.residual = q.x[now];
             g.residual_row = q.x_row;
@@ -771,7 +783,7 @@ int run_schulz(Stream& s, std::vector<SchulzGroup>& groups, int steps, int plane
           }
           p.group[k] = g;
         }
-        OP_DO(run_products(s, p, batches, false, phase == 0 ? kGram : phase == 1 ? kPolynomial : final ? last_epilogue : kUpdate));
+        OP_DO(run_products(s, p, factors, phase == 0 ? kGram : phase == 1 ? kPolynomial : final ? last_epilogue : kUpdate));
       }
     }
   }
@@ -876,7 +888,7 @@ int netmax_orthogonalise(const netmax_orthogonal* o) try {
   const dim3 grid((unsigned)blocks_of(room.sweep), (unsigned)std::min(o->count, 32768));
   OP_DO(launch(s, f32 ? norm_parts_kernel<float> : norm_parts_kernel<__nv_bfloat16>, grid, kElementThreads, 0, 1, np));
   OP_DO(launch(s, f32 ? first_iterate_kernel<float> : first_iterate_kernel<__nv_bfloat16>, grid, kElementThreads, 0, 1, np));
-  OP_DO(q.encode_maps(planes_of(o->storage)));
+  q.describe(planes_of(o->storage));
   std::vector<SchulzGroup> groups(1, q);
   ProductParams p;
   return run_schulz(s, groups, o->steps, planes_of(o->storage), f32 ? kLastF32 : kLastBf16, p, [&](size_t, ProductGroup& g) {
@@ -1072,7 +1084,7 @@ int enqueue_step(const netmax_step& t, int draw_stride, unsigned int* error, int
         p.matrix_offset[at] = (uint32_t)plan.sorted[at].offset;
         p.matrix_scale[at] = (float)plan.sorted[at].scale;
       }
-      OP_DO(g.encode_maps(planes_of(t.storage)));
+      g.describe(planes_of(t.storage));
     }
     OP_DO(launch(s, f32 ? step_first_iterate_kernel<float> : step_first_iterate_kernel<__nv_bfloat16>, grid, kElementThreads, 0, 1, sp, tables));
     p.step = sp.pull;

@@ -60,6 +60,7 @@ struct ProductGroup {
   int32_t M = 0, N = 0, K = 0;
   int32_t symmetric = 0;       // tiles on and below the diagonal, the others mirrored
   int32_t a_mn = 0, b_mn = 0;  // m (n) contiguous instead of k
+  int32_t a_box = 64, b_box = 64;  // rows of a box
   int32_t bn = 0;              // columns of a tile
   int32_t a_batched = 1, b_batched = 1;  // 0: one matrix for all
   uint32_t idesc = 0;
@@ -623,9 +624,9 @@ __global__ __launch_bounds__(product_threads(kPlanes), 1) void product_kernel(co
         const uint32_t bar = kCtas == 2 ? ptx::map_to(full + 8 * s, 0) : full + 8 * s;
         const uint32_t at = base + s * p.stage_bytes;
         for (int plane = 0; plane < kPlanes; ++plane) {
-          for (int b = 0; b < 2; ++b)
+          for (int b = 0; b < 2; b += g.a_box / 64)
             ptx::load_box<kCtas>(at + plane * p.a_bytes + b * kBoxBytes, &g.a, bar, g.a_mn ? m0 + 64 * b : kb * 64, g.a_mn ? kb * 64 : m0 + 64 * b, qa, plane);
-          for (int b = 0; b < boxes_b; ++b)
+          for (int b = 0; b < boxes_b; b += g.b_box / 64)
             ptx::load_box<kCtas>(at + kPlanes * p.a_bytes + plane * p.b_bytes + b * kBoxBytes, &g.b, bar, g.b_mn ? n0 + 64 * b : kb * 64,
                                  g.b_mn ? kb * 64 : n0 + 64 * b, qb, plane);
         }
