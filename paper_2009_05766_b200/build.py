@@ -14,7 +14,8 @@ SOURCES = ["netmax.cu", "netmax_fused.cu", "netmax_tiles_f32.cu", "netmax_tiles_
            "netmax_operators.cu"]
 HEADERS = ["netmax_policy_gpu_host.inc", "netmax_tile_instances.inc", "netmax_instances.h", "netmax_kernels.cuh", "netmax_plain.cuh", "netmax_tiles.cuh",
            "netmax_pipe.cuh", "netmax_rng.cuh", "netmax_fp64.cuh", "netmax_search.h", "netmax_policy.h", "netmax_bulk.h",
-           "netmax_operators.cuh", "netmax_operators.h", "netmax_product.cuh", "netmax_small.cuh", os.path.join("..", "..", "include", "netmax.h")]
+           "netmax_operators.cuh", "netmax_operators.h", "netmax_product.cuh", "netmax_small.cuh", "netmax_few_rows.cuh",
+           os.path.join("..", "..", "include", "netmax.h")]
 DEPS = SOURCES + HEADERS
 
 

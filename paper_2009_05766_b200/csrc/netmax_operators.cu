@@ -12,6 +12,7 @@
 #include <unordered_map>
 #include <vector>
 
+#include "netmax_few_rows.cuh"
 #include "netmax_operators.cuh"
 #include "netmax_operators.h"
 #include "netmax_policy.h"
@@ -201,22 +202,6 @@ ProductKernel pick_product(int epilogue, int planes) {
   }
 }
 
-// The kernels for two planes share their registers out anew (216 a thread for the epilogue, 72 for the others), which waits for good
-// where a launch did not get that many: a build that gave such a kernel fewer than 168 is refused.
-int check_registers(const void* kernel) {
-  static std::mutex mu;
-  static auto* known = new std::unordered_map<const void*, int>();
-  std::lock_guard<std::mutex> lock(mu);
-  int& registers = (*known)[kernel];
-  if (registers == 0) {
-    cudaFuncAttributes a;
-    OP_CUDA(cudaFuncGetAttributes(&a, kernel));
-    registers = a.numRegs;
-  }
-  if (registers * product_threads(2) < (2 * 216 + 72) * 128) return fail_op(NETMAX_CUDA_ERROR, "a product kernel was built with %d registers, 168 needed", registers);
-  return NETMAX_OK;
-}
-
 // What a group of a launch multiplies.
 struct Factors {
   const Operand *a = nullptr, *b = nullptr;
@@ -236,12 +221,14 @@ int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilog
   const int sms = sm_count();
   auto tiles_of = [&](const ProductGroup& g, int batch, int tile_m, int bn) {
     const int64_t tm = ceil_div(g.M, tile_m), tn = ceil_div(g.N, bn);
-    return (int64_t)batch * (g.symmetric ? tm * (tm + 1) / 2 : tm * tn);
+    return (int64_t)batch * (g.symmetric ? tile_m / bn * (tm * (tm - 1) / 2) + tn : tm * tn);
   };
+  // Columns of a pair's tile: 256 with one plane, 128 with two (and of narrow outputs; symmetric ones never have more columns than rows).
+  auto pair_columns = [&](const ProductGroup& g) { return p.planes == 2 || (!g.symmetric && g.N <= 128) ? 128 : 256; };
   int64_t pairs = 0, wide = 0;
   for (int k = 0; k < p.groups; ++k) {
     const ProductGroup& g = p.group[k];
-    pairs += tiles_of(g, factors[k].batch, 256, g.symmetric || g.N > 128 ? 256 : 128);
+    pairs += tiles_of(g, factors[k].batch, 256, pair_columns(g));
     wide += tiles_of(g, factors[k].batch, 128, 128);
   }
   const int ctas = pairs * 5 >= sms / 2 * 4 ? 2 : 1;
@@ -249,10 +236,11 @@ int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilog
   int most_b = 0;
   for (int k = 0; k < p.groups; ++k) {
     ProductGroup& g = p.group[k];
-    if (ctas == 2) g.bn = g.symmetric || g.N > 128 ? 256 : 128;
+    if (ctas == 2) g.bn = pair_columns(g);
     else g.bn = g.symmetric ? 128 : g.N <= 64 || wide * 2 <= sms ? 64 : 128;
     g.tiles_m = ceil_div(g.M, 128 * ctas);
     g.tiles_n = ceil_div(g.N, g.bn);
+    if (g.symmetric) g.symmetric = 128 * ctas / g.bn;
     g.tile_begin = (int)tiles;
     tiles += tiles_of(g, factors[k].batch, 128 * ctas, g.bn);
     // the longer a box, the fewer of them: 128 rows of a k-contiguous operand (8 x 4096^3: 950 us with boxes of 64, 880 so)
@@ -270,16 +258,15 @@ int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilog
   p.a_bytes = 128 * 128;
   p.b_bytes = (uint32_t)most_b * 128;
   p.stage_bytes = (uint32_t)p.planes * (p.a_bytes + p.b_bytes);
-  const size_t slots = (size_t)epilogue_warps(p.planes) * kSlotBytes;
+  const size_t slots = (size_t)kEpilogueWarps * kSlotBytes;
   p.stages = (int)std::min<size_t>(kMaxStages, (kProductSmem - 1024 - slots) / p.stage_bytes);
   const size_t smem = std::max(kLeastSmem, (size_t)1024 + slots + (size_t)p.stages * p.stage_bytes);
   p.error = s.error;
   p.clear_error = s.clear;
   ProductKernel kernel = ctas == 2 ? pick_product<2>(epilogue, p.planes) : pick_product<1>(epilogue, p.planes);
   OP_CUDA(raise_smem_limit((const void*)kernel, smem));
-  if (p.planes == 2) OP_DO(check_registers((const void*)kernel));
   const int grid = (int)std::min<int64_t>(tiles, sms / ctas) * ctas;
-  OP_DO(launch(s, kernel, dim3(grid), product_threads(p.planes), smem, ctas, p));
+  OP_DO(launch(s, kernel, dim3(grid), kProductThreads, smem, ctas, p));
   s.clear = false;
   return NETMAX_OK;
 }
@@ -415,6 +402,58 @@ int run_jobs(Stream& s, OperandParams& jobs, int n_jobs, int storage) {
   return launch(s, storage == NETMAX_STORAGE_F32 ? operand_kernel<float> : operand_kernel<__nv_bfloat16>, grid, kElementThreads, 0, 1, jobs);
 }
 
+int few_rows(Stream& s, const netmax_layer& l) {
+  FewRowsParams p;
+  p.x = l.x.data;
+  p.x_row = l.x.row_stride;
+  p.x_batch = l.x.worker_stride;
+  p.weight = l.weight.data;
+  p.weight_row = l.weight.row_stride;
+  p.weight_batch = l.weight.worker_stride;
+  p.bias = l.bias.data;
+  p.bias_batch = l.bias.worker_stride;
+  p.residual = l.residual.data;
+  p.residual_row = l.residual.row_stride;
+  p.residual_batch = l.residual.worker_stride;
+  p.y = l.y.data;
+  p.y_row = l.y.row_stride;
+  p.y_batch = l.y.worker_stride;
+  p.z = l.z.data;
+  p.z_row = l.z.row_stride;
+  p.z_batch = l.z.worker_stride;
+  p.n = (int32_t)l.n;
+  p.n_in = (int32_t)l.n_in;
+  p.n_out = (int32_t)l.n_out;
+  p.activation = l.activation;
+  p.error = s.error;
+  const bool f32 = l.storage == NETMAX_STORAGE_F32;
+  const int64_t unit = f32 ? 4 : 8;
+  auto fits = [&](const netmax_view& v, int64_t rows) {
+    return ((uintptr_t)v.data & 15) == 0 && (rows == 1 || v.row_stride % unit == 0) && (l.M == 1 || v.worker_stride % unit == 0);
+  };
+  p.pieces = fits(l.x, l.n) && fits(l.weight, l.n_out);
+  const int rows = l.n <= 1 ? 1 : l.n <= 2 ? 2 : l.n <= 4 ? 4 : 8;
+  // two outputs a warp share the loads of x; one where that would leave SMs without work
+  const bool two = l.M * ceil_div<int64_t>(l.n_out, 16) >= sm_count();
+  const dim3 grid((unsigned)ceil_div<int64_t>(l.n_out, two ? 16 : 8), (unsigned)l.M);
+  auto run = [&](void (*kernel)(const FewRowsParams)) { return launch(s, kernel, grid, kElementThreads, 0, 1, p); };
+  if (f32) {
+    switch (rows) {
+      case 1: return run(two ? few_rows_kernel<float, 1, 2> : few_rows_kernel<float, 1, 1>);
+      case 2: return run(two ? few_rows_kernel<float, 2, 2> : few_rows_kernel<float, 2, 1>);
+      case 4: return run(two ? few_rows_kernel<float, 4, 2> : few_rows_kernel<float, 4, 1>);
+      default: return run(two ? few_rows_kernel<float, 8, 2> : few_rows_kernel<float, 8, 1>);
+    }
+  }
+  using B = __nv_bfloat16;
+  switch (rows) {
+    case 1: return run(two ? few_rows_kernel<B, 1, 2> : few_rows_kernel<B, 1, 1>);
+    case 2: return run(two ? few_rows_kernel<B, 2, 2> : few_rows_kernel<B, 2, 1>);
+    case 4: return run(two ? few_rows_kernel<B, 4, 2> : few_rows_kernel<B, 4, 1>);
+    default: return run(two ? few_rows_kernel<B, 8, 2> : few_rows_kernel<B, 8, 1>);
+  }
+}
+
 // One product of a launch: D[m][n] over k.
 void fill_product(ProductGroup& g, const Prepared& a, bool a_mn, const Prepared& b, bool b_mn, int64_t M, int64_t N, int64_t K) {
   g.M = (int32_t)M;
@@ -548,6 +587,7 @@ int netmax_layer_forward(const netmax_layer* l) try {
     OP_CUDA(cudaMemsetAsync(l->workspace, 0, 4, s.stream));
     return NETMAX_OK;
   }
+  if (n <= kFewRows) return few_rows(s, *l);
   OperandParams jobs;
   int n_jobs = 0;
   const Prepared w = prepare_operand(l->weight, nullptr, 0, l->M, n_out, n_in, l->storage, room.weight, jobs, n_jobs);

@@ -329,8 +329,8 @@ __device__ __forceinline__ int find_segment(const StepParams& p, uint32_t piece)
   return lo;
 }
 
-// A piece of a segment: elements [first, last), taken eight at a time from the multiple of eight at or before `first` on, so that every
-// full group lies on a 16-byte boundary where the arrays do.
+// A piece of a segment: elements [first, last), taken four at a time from the multiple of eight at or before `first` on, so that every
+// full group lies on a 16-byte boundary where fp32 arrays do (and a warp's stores fill whole sectors).
 struct Piece {
   uint32_t first, last, group;
 };
@@ -339,24 +339,24 @@ __device__ __forceinline__ Piece piece_of(const StepSegment& s, uint32_t block) 
   const uint32_t base = s.offset & ~7u, begin = base + (block - s.first_piece) * kPiece;
   p.first = max(begin, s.offset);
   p.last = min(begin + kPiece, s.offset + s.length);
-  p.group = begin + threadIdx.x * 8;
+  p.group = begin + threadIdx.x * 4;
   return p;
 }
-// Eight elements from `at` on, of which those in [first, last) exist.
+// Four elements from `at` on, of which those in [first, last) exist.
 template <typename T>
-__device__ __forceinline__ void load_group(const T* base, uint32_t at, const Piece& p, float (&v)[8]) {
-  if (at >= p.first && at + 8 <= p.last) return load8(base + at, 8, v);
+__device__ __forceinline__ void load_group(const T* base, uint32_t at, const Piece& p, float (&v)[4]) {
+  if (at >= p.first && at + 4 <= p.last) return load_values<T, false, 4>(base + at, 4, v);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) v[k] = at + k >= p.first && at + k < p.last ? (float)base[at + k] : 0.0f;
+  for (int k = 0; k < 4; ++k) v[k] = at + k >= p.first && at + k < p.last ? (float)base[at + k] : 0.0f;
 }
 template <typename T>
-__device__ __forceinline__ void store_group(T* base, uint32_t at, const Piece& p, const float (&v)[8]) {
-  if (at >= p.first && at + 8 <= p.last) return store8(base + at, 8, v);
+__device__ __forceinline__ void store_group(T* base, uint32_t at, const Piece& p, const float (&v)[4]) {
+  if (at >= p.first && at + 4 <= p.last) return store_values<T, false, 4>(base + at, 4, v);
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
+  for (int k = 0; k < 4; ++k)
     if (at + k >= p.first && at + k < p.last) base[at + k] = (T)v[k];
 }
-constexpr int kGroupsPerThread = kPiece / (8 * kElementThreads);
+constexpr int kGroupsPerThread = kPiece / (4 * kElementThreads);
 
 // m' = mu m + g, u = g + mu m' or m'; sums of squares of u inside matrices, the whole update outside them.
 template <typename T>
@@ -371,20 +371,20 @@ __global__ __launch_bounds__(kElementThreads) void step_momentum_kernel(const __
     const float* m = p.momentum + i * p.momentum_row;
     float* m_next = p.momentum_next + i * p.momentum_next_row;
     double s = 0.0;
-    float grad[kGroupsPerThread][8], mom[kGroupsPerThread][8];
+    float grad[kGroupsPerThread][4], mom[kGroupsPerThread][4];
 #pragma unroll
     for (int u = 0; u < kGroupsPerThread; ++u) {
-      const uint32_t at = piece.group + u * 8 * kElementThreads;
+      const uint32_t at = piece.group + u * 4 * kElementThreads;
       if (at >= piece.last) break;
       load_group(g, at, piece, grad[u]);
       load_group(m, at, piece, mom[u]);
     }
 #pragma unroll
     for (int u = 0; u < kGroupsPerThread; ++u) {
-      const uint32_t at = piece.group + u * 8 * kElementThreads;
+      const uint32_t at = piece.group + u * 4 * kElementThreads;
       if (at >= piece.last) break;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
+      for (int k = 0; k < 4; ++k) {
         mom[u][k] = fmaf(p.mu, mom[u][k], grad[u][k]);
         grad[u][k] = p.nesterov ? fmaf(p.mu, mom[u][k], grad[u][k]) : mom[u][k];  // (elements outside the piece are zeros)
         s += (double)grad[u][k] * (double)grad[u][k];
@@ -404,13 +404,13 @@ __global__ __launch_bounds__(kElementThreads) void step_momentum_kernel(const __
     T* next = (T*)p.pull.x_next + i * p.pull.next_row;
 #pragma unroll
     for (int u = 0; u < kGroupsPerThread; ++u) {
-      const uint32_t at = piece.group + u * 8 * kElementThreads;
+      const uint32_t at = piece.group + u * 4 * kElementThreads;
       if (at >= piece.last) break;
-      float x[8], xm[8];
+      float x[4], xm[4];
       load_group(own, at, piece, x);
       load_group(other, at, piece, xm);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
+      for (int k = 0; k < 4; ++k) {
         const float h = fmaf(-p.pull.lr, fmaf(p.pull.decay, x[k], grad[u][k]), x[k]);
         x[k] = pull ? fmaf(-w, h - xm[k], h) : h;
       }
@@ -427,14 +427,14 @@ __global__ __launch_bounds__(kElementThreads) void step_first_iterate_kernel(con
   const StepMatrix& to = tables.matrix[seg.matrix];
   const Piece piece = piece_of(seg, blockIdx.x);
   const uint32_t pieces = ((seg.offset & 7) + seg.length + kPiece - 1) / kPiece, cols = to.cols;
-  const bool whole = ((seg.offset | cols) & 7) == 0;  // groups of eight do not cross rows
+  const bool whole = ((seg.offset | cols) & 3) == 0;  // groups of four do not cross rows
   for (int i = blockIdx.y; i < p.workers; i += gridDim.y) {
     const T* g = (const T*)p.gradient + i * p.gradient_row;
     const float* m_next = p.momentum_next + i * p.momentum_next_row;
-    float grad[kGroupsPerThread][8], mom[kGroupsPerThread][8];
+    float grad[kGroupsPerThread][4], mom[kGroupsPerThread][4];
 #pragma unroll
     for (int u = 0; u < kGroupsPerThread; ++u) {
-      const uint32_t at = piece.group + u * 8 * kElementThreads;
+      const uint32_t at = piece.group + u * 4 * kElementThreads;
       if (at >= piece.last) break;
       load_group(m_next, at, piece, mom[u]);
       if (p.nesterov) load_group(g, at, piece, grad[u]);
@@ -445,27 +445,27 @@ __global__ __launch_bounds__(kElementThreads) void step_first_iterate_kernel(con
     __half* planes = to.planes + i * to.worker;
 #pragma unroll
     for (int u = 0; u < kGroupsPerThread; ++u) {
-      const uint32_t at = piece.group + u * 8 * kElementThreads;
+      const uint32_t at = piece.group + u * 4 * kElementThreads;
       if (at >= piece.last) break;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) mom[u][k] = (p.nesterov ? fmaf(p.mu, mom[u][k], grad[u][k]) : mom[u][k]) * inverse.a * inverse.b;
-      uint4 hi, lo;
-      split8(mom[u], hi, lo);
-      if (whole) {  // (then the piece's ends are multiples of eight, too)
+      for (int k = 0; k < 4; ++k) mom[u][k] = (p.nesterov ? fmaf(p.mu, mom[u][k], grad[u][k]) : mom[u][k]) * inverse.a * inverse.b;
+      uint32_t hi[2], lo[2];
+      split_values<4>(mom[u], hi, lo);
+      if (whole) {  // (then a group lies inside the segment or outside it)
+        if (at < piece.first) continue;
         const uint32_t e = at - seg.offset, row = e / cols;
-        __half* to8 = planes + row * to.row + (e - row * cols);
-        *(uint4*)to8 = hi;
-        *(uint4*)(to8 + to.plane) = lo;
+        __half* to4 = planes + row * to.row + (e - row * cols);
+        store_words(to4, hi);
+        store_words(to4 + to.plane, lo);
       } else {
-        const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
         const uint32_t begin = max(at, piece.first) - seg.offset;
         uint32_t row = begin / cols, col = begin - row * cols;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < 4; ++k) {
           if (at + k < piece.first || at + k >= piece.last) continue;
           __half* to1 = planes + row * to.row + col;
-          to1[0] = __ushort_as_half((unsigned short)(h[k / 2] >> (16 * (k % 2))));
-          to1[to.plane] = __ushort_as_half((unsigned short)(l[k / 2] >> (16 * (k % 2))));
+          to1[0] = __ushort_as_half((unsigned short)(hi[k / 2] >> (16 * (k % 2))));
+          to1[to.plane] = __ushort_as_half((unsigned short)(lo[k / 2] >> (16 * (k % 2))));
           if (++col == cols) {
             col = 0;
             ++row;

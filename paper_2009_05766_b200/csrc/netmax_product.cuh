@@ -9,9 +9,12 @@
 //   hi hi + hi lo + lo hi = s^2 A B^T (1 + O(2^-22))
 // costs three products in one accumulator instead of one (the term lo lo is below the fp32 accumulator's own rounding).
 //
-// One CTA pair (cta_group::2) works on a tile of 256 x up to 256, each CTA with its own 128 rows of A and half the rows of B in
-// shared memory: a tile of k = 64 then costs an SM 32 KB from L2 for 512 cycles of tensor work, 48 KB if every CTA worked for
-// itself.  Problems that would leave SMs without a tile that way take one CTA per tile of 128 x 64 to 128 x 256.  The first warps are the
+// One CTA pair (cta_group::2) works on a tile of 256 x 256 (two planes: 256 x 128), each CTA with its own 128 rows of A and half the rows
+// of B in shared memory: a tile of k = 64 then costs an SM 32 KB from L2 for 512 cycles of tensor work, 48 KB if every CTA worked for
+// itself.  Problems that would leave SMs without a tile that way take one CTA per tile of 128 x 64 or 128 x 128.  With two planes the epilogue
+// warps hold fp32 sums (see kPromote): of 128 columns they are 32 registers a thread, and sixteen warps finish a tile under the
+// products of the next; of 256 columns eight warps held 128 each and the tensor cores waited for them (fp32 layer of 8 x (512 x 512 x 2048):
+// 50 us).  The first warps are the
 // epilogue, one issues the TMA loads, one the products; the accumulators are double-buffered so that the epilogue of a tile
 // runs under the products of the next.
 //
@@ -31,16 +34,16 @@
 
 namespace netmax {
 
-// Epilogue warps: sixteen where a thread holds one chunk, eight where it holds sums of 128 columns.  Behind them one warp loads, one
-// multiplies and two fill their warpgroup.
-__host__ __device__ constexpr int epilogue_warps(int planes) { return planes == 1 ? 16 : 8; }
-__host__ __device__ constexpr int product_threads(int planes) { return (epilogue_warps(planes) + 4) * 32; }
+constexpr int kEpilogueWarps = 16;        // behind them one warp loads and one multiplies
+constexpr int kProductThreads = (kEpilogueWarps + 2) * 32;
 constexpr int kSlotBytes = 4096;          // of an epilogue warp: 32 x 32 fp32
 constexpr int kProductBox = 64;           // a TMA box: 64 rows of 64 16-bit values (128 bytes, the swizzle's width)
 constexpr int kBoxBytes = kProductBox * 128;
 constexpr int kMaxGroups = 12;            // groups of equal matrices in one launch
 constexpr int kMaxMatrices = 256;         // matrices of one replica in one launch
 constexpr int kMaxStages = 8;
+// Accumulators in TMEM's 512 columns: two of 256, or four of 128.
+__host__ __device__ constexpr int accumulators(int planes) { return planes == 2 ? 4 : 2; }
 constexpr float kPlaneScale = 16384.0f;   // 2^14: what the planes of Newton-Schulz iterates are scaled by (all |v| < 2.9)
 constexpr float kPlaneUnscale = 1.0f / 16384.0f;
 
@@ -58,7 +61,7 @@ struct ProductGroup {
   CUtensorMap a, b;  // {contiguous, other, matrix, plane}
   int32_t tile_begin = 0, tiles_m = 0, tiles_n = 0;
   int32_t M = 0, N = 0, K = 0;
-  int32_t symmetric = 0;       // tiles on and below the diagonal, the others mirrored
+  int32_t symmetric = 0;       // only tiles up to the diagonal, the others mirrored: a tile's rows over its columns (1 or 2); 0: no
   int32_t a_mn = 0, b_mn = 0;  // m (n) contiguous instead of k
   int32_t a_box = 64, b_box = 64;  // rows of a box
   int32_t bn = 0;              // columns of a tile
@@ -133,19 +136,13 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
                : "=r"(done) : "r"(bar), "r"(parity) : "memory");
   return done != 0;
 }
-__device__ __forceinline__ uint64_t now_ns() {
-  uint64_t t;
-  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-  return t;
-}
-// False if the phase did not end within two seconds (or 2^26 looks, whichever comes first).
+// False if the phase did not end within 2^32 cycles (about two seconds) or 2^28 looks, whichever comes first.
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
-  for (int i = 0; i < 64; ++i)
+  if (try_wait(bar, parity)) return true;
+  const long long start = clock64();
+  for (uint32_t i = 0; i < (1u << 28); ++i) {
     if (try_wait(bar, parity)) return true;
-  const uint64_t start = now_ns();
-  for (uint32_t i = 0; i < (1u << 26); ++i) {
-    if (try_wait(bar, parity)) return true;
-    if ((i & 255) == 255 && now_ns() - start > 2000000000ull) return false;
+    if ((i & 1023) == 1023 && clock64() - start > (1ll << 32)) return false;
   }
   return false;
 }
@@ -234,130 +231,166 @@ __device__ __forceinline__ float activation_slope(float z, int activation) {
   const float s = __fdividef(1.0f, 1.0f + __expf(-z));
   return s * (1.0f + z * (1.0f - s));
 }
-// The two fp16 planes of a scaled value; what is not finite stays so, once.
-__device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
-  hi = __float2half_rn(v);
-  const float h = __half2float(hi);
-  lo = fabsf(h) <= 65504.0f ? __float2half_rn(v - h) : __float2half_rn(0.0f);
-}
-
 struct Tile {
   int g, q, i, j;  // group, matrix, tile row (m) and column (n)
 };
 __device__ __forceinline__ Tile find_tile(const ProductParams& p, int t) {
-  Tile r;
-  r.g = 0;
-  while (r.g + 1 < p.groups && p.group[r.g + 1].tile_begin <= t) ++r.g;
-  const ProductGroup& g = p.group[r.g];
+  Tile out;
+  out.g = 0;
+  while (out.g + 1 < p.groups && p.group[out.g + 1].tile_begin <= t) ++out.g;
+  const ProductGroup& g = p.group[out.g];
   t -= g.tile_begin;
-  if (g.symmetric) {
-    const int per = g.tiles_m * (g.tiles_m + 1) / 2;
-    r.q = t / per;
-    t -= r.q * per;
-    int i = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);  // (at most one off: i is small)
-    while (i * (i + 1) / 2 > t) --i;
-    while ((i + 1) * (i + 2) / 2 <= t) ++i;
-    r.i = i;
-    r.j = t - i * (i + 1) / 2;
+  if (g.symmetric) {  // row i has the tiles up to the diagonal's: (i + 1) r, the last row as many as there are
+    const int r = g.symmetric, per = r * (g.tiles_m * (g.tiles_m - 1) / 2) + g.tiles_n;
+    out.q = t / per;
+    t -= out.q * per;
+    int i = (int)((sqrtf(8.0f * (float)(t / r) + 1.0f) - 1.0f) * 0.5f);  // (at most one off: i is small)
+    while (r * (i * (i + 1) / 2) > t) --i;
+    while (r * ((i + 1) * (i + 2) / 2) <= t) ++i;
+    out.i = i;
+    out.j = t - r * (i * (i + 1) / 2);
   } else {
     const int per = g.tiles_m * g.tiles_n;
-    r.q = t / per;
-    t -= r.q * per;
-    r.j = t / g.tiles_m;
-    r.i = t - r.j * g.tiles_m;
+    out.q = t / per;
+    t -= out.q * per;
+    out.j = t / g.tiles_m;
+    out.i = t - out.j * g.tiles_m;
   }
-  return r;
+  return out;
 }
 
-// Eight values of a type, in 16-byte pieces where the address allows it (kWhole: it does); `count` of them exist.
-template <typename T, bool kWhole = false>
-__device__ __forceinline__ void load8(const T* at, int count, float (&v)[8]) {
-  if (kWhole || (count == 8 && ((uintptr_t)at & 15) == 0)) {
+// Two or four words of packed 16-bit values.
+template <int kWords>
+__device__ __forceinline__ void load_words(const void* at, uint32_t (&w)[kWords]) {
+  if constexpr (kWords == 4) {
+    const uint4 a = *(const uint4*)at;
+    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+  } else {
+    const uint2 a = *(const uint2*)at;
+    w[0] = a.x, w[1] = a.y;
+  }
+}
+template <int kWords>
+__device__ __forceinline__ void store_words(void* at, const uint32_t (&w)[kWords]) {
+  if constexpr (kWords == 4) *(uint4*)at = make_uint4(w[0], w[1], w[2], w[3]);
+  else *(uint2*)at = make_uint2(w[0], w[1]);
+}
+// kN values of a type (four or eight), in pieces of up to 16 bytes where the address allows it (kWhole: it does); `count` of them exist.
+template <typename T, bool kWhole, int kN>
+__device__ __forceinline__ void load_values(const T* at, int count, float (&v)[kN]) {
+  constexpr int kPieceBytes = kN * (int)sizeof(T) < 16 ? kN * (int)sizeof(T) : 16;
+  if (kWhole || (count == kN && ((uintptr_t)at & (kPieceBytes - 1)) == 0)) {
     if (sizeof(T) == 4) {
-      const float4 a = ((const float4*)at)[0], b = ((const float4*)at)[1];
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    } else {
-      const uint4 a = *(const uint4*)at;
-      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < kN; k += 4) {
+        const float4 a = *(const float4*)(at + k);
+        v[k] = a.x, v[k + 1] = a.y, v[k + 2] = a.z, v[k + 3] = a.w;
+      }
+    } else {
+      uint32_t w[kN / 2];
+      load_words(at, w);
+#pragma unroll
+      for (int k = 0; k < kN / 2; ++k) {
         v[2 * k] = __uint_as_float(w[k] << 16);
         v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
       }
     }
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = k < count ? (float)at[k] : 0.0f;
+    for (int k = 0; k < kN; ++k) v[k] = k < count ? (float)at[k] : 0.0f;
   }
 }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *(const uint32_t*)&h;
 }
-template <typename T, bool kWhole = false>
-__device__ __forceinline__ void store8(T* at, int count, const float (&v)[8]) {
-  if (kWhole || (count == 8 && ((uintptr_t)at & 15) == 0)) {
+template <typename T, bool kWhole, int kN>
+__device__ __forceinline__ void store_values(T* at, int count, const float (&v)[kN]) {
+  constexpr int kPieceBytes = kN * (int)sizeof(T) < 16 ? kN * (int)sizeof(T) : 16;
+  if (kWhole || (count == kN && ((uintptr_t)at & (kPieceBytes - 1)) == 0)) {
     if (sizeof(T) == 4) {
-      ((float4*)at)[0] = make_float4(v[0], v[1], v[2], v[3]);
-      ((float4*)at)[1] = make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+      for (int k = 0; k < kN; k += 4) *(float4*)(at + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
     } else {
-      *(uint4*)at = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+      uint32_t w[kN / 2];
+#pragma unroll
+      for (int k = 0; k < kN / 2; ++k) w[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
+      store_words(at, w);
     }
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
+    for (int k = 0; k < kN; ++k)
       if (k < count) at[k] = (T)v[k];
   }
 }
-__device__ __forceinline__ void unpack_half(const uint4& a, float (&v)[8]) {
-  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+template <typename T>
+__device__ __forceinline__ void load8(const T* at, int count, float (&v)[8]) { load_values<T, false, 8>(at, count, v); }
+template <typename T>
+__device__ __forceinline__ void store8(T* at, int count, const float (&v)[8]) { store_values<T, false, 8>(at, count, v); }
+
+// Words of two fp16 each.
+template <int kN>
+__device__ __forceinline__ void unpack_half(const uint32_t (&w)[kN / 2], float (&v)[kN]) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < kN / 2; ++k) {
     const float2 f = __half22float2(*(const __half2*)&w[k]);
     v[2 * k] = f.x;
     v[2 * k + 1] = f.y;
   }
 }
-__device__ __forceinline__ uint4 half8(const float (&v)[8]) {
-  uint32_t h[4];
+template <int kN>
+__device__ __forceinline__ void pack_half(const float (&v)[kN], uint32_t (&w)[kN / 2]) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < kN / 2; ++k) {
     const __half2 a = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
-    h[k] = *(const uint32_t*)&a;
+    w[k] = *(const uint32_t*)&a;
   }
-  return make_uint4(h[0], h[1], h[2], h[3]);
 }
-// Eight values as two planes.
-__device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {
-  uint32_t h[4], l[4];
+// Values as two planes; what is not finite stays so, once.
+template <int kN>
+__device__ __forceinline__ void split_values(const float (&v)[kN], uint32_t (&hi)[kN / 2], uint32_t (&lo)[kN / 2]) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < kN / 2; ++k) {
     const __half2 a = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
     const float2 f = __half22float2(a);
     const __half2 b = __floats2half2_rn(fabsf(f.x) <= 65504.0f ? v[2 * k] - f.x : 0.0f, fabsf(f.y) <= 65504.0f ? v[2 * k + 1] - f.y : 0.0f);
-    h[k] = *(const uint32_t*)&a;
-    l[k] = *(const uint32_t*)&b;
+    hi[k] = *(const uint32_t*)&a;
+    lo[k] = *(const uint32_t*)&b;
   }
+}
+__device__ __forceinline__ void unpack_half(const uint4& a, float (&v)[8]) {
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+  unpack_half<8>(w, v);
+}
+__device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {
+  uint32_t h[4], l[4];
+  split_values<8>(v, h, l);
   hi = make_uint4(h[0], h[1], h[2], h[3]);
   lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
+// Columns that a lane takes of a row of a staged chunk: eight where 16-bit values are stored, four where fp32 is (16 bytes either way;
+// with eight, two stores would each fill halves of their sectors).  32 / kN lanes a row, kN rows at a time, 32 / kN times.
+__host__ __device__ constexpr int lane_columns(int epilogue) { return epilogue == kLayerF32 || epilogue == kLastF32 || epilogue == kStepF32 ? 4 : 8; }
 
-// What an epilogue reads besides the accumulator: rows i * 8 + lane / 4, columns 8 (lane % 4) ... of a chunk, both planes.
+// What an epilogue reads besides the accumulator, both planes, as it will go over the chunk.
+template <int kN>
 struct Residual {
-  uint4 hi[4], lo[4];
+  uint32_t hi[32 / kN][kN / 2], lo[32 / kN][kN / 2];
 };
 template <int kEpilogue, int kPlanes>
-__device__ __forceinline__ void load_residual(const ProductGroup& g, int q, int m0, int n0, int lane, Residual& r) {
-  if (kEpilogue < kPolynomial) return;
-  const int n = n0 + 8 * (lane % 4), row = lane / 4, rows = n < g.N ? g.M - m0 - row : 0;  // (planes' rows are padded to eight columns)
+__device__ __forceinline__ void load_residual(const ProductGroup& g, int q, int m0, int n0, int lane, Residual<lane_columns(kEpilogue)>& r) {
+  if (kEpilogue < kPolynomial || kEpilogue >= kStepF32) return;  // (the step reads them along with the replicas)
+  constexpr int kN = lane_columns(kEpilogue), kLanes = 32 / kN;
+  const int n = n0 + kN * (lane % kLanes), row = lane / kLanes, rows = n < g.N ? g.M - m0 - row : 0;  // (planes' rows are padded to eight columns)
   const __half* at = (const __half*)g.residual + q * g.residual_batch + (int64_t)(m0 + row) * g.residual_row + n;
-  const int64_t step = 8 * g.residual_row;
+  const int64_t step = kN * g.residual_row;
 #pragma unroll
-  for (int i = 0; i < 4; ++i, at += step) {
-    r.hi[i] = r.lo[i] = make_uint4(0, 0, 0, 0);
-    if (8 * i < rows) {
-      r.hi[i] = *(const uint4*)at;
-      if (kEpilogue > kPolynomial || kPlanes == 2) r.lo[i] = *(const uint4*)(at + g.residual_plane);
+  for (int i = 0; i < 32 / kN; ++i, at += step) {
+#pragma unroll
+    for (int k = 0; k < kN / 2; ++k) r.hi[i][k] = r.lo[i][k] = 0;
+    if (kN * i < rows) {
+      load_words(at, r.hi[i]);
+      if (kEpilogue > kPolynomial || kPlanes == 2) load_words(at + g.residual_plane, r.lo[i]);
     }
   }
 }
@@ -371,33 +404,39 @@ __device__ __forceinline__ void stage_row(float* slot, const float (&acc)[32]) {
     *(float4*)(slot + lane * 32 + (c ^ (lane & 7)) * 4) = make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
 }
 
-__device__ __forceinline__ void activate8(float (&v)[8], int activation) {
+template <int kN>
+__device__ __forceinline__ void activate_all(float (&v)[kN], int activation) {
   if (activation == kActRelu) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = activate(v[k], kActRelu);
+    for (int k = 0; k < kN; ++k) v[k] = activate(v[k], kActRelu);
   } else if (activation == kActGelu) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = activate(v[k], kActGelu);
+    for (int k = 0; k < kN; ++k) v[k] = activate(v[k], kActGelu);
   } else if (activation == kActSilu) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = activate(v[k], kActSilu);
+    for (int k = 0; k < kN; ++k) v[k] = activate(v[k], kActSilu);
   }
 }
-// A lane's eight columns of row `row` of the staged chunk.
-__device__ __forceinline__ void read_slot(const float* slot, int row, int c, float (&v)[8]) {
-  const float4 a = *(const float4*)(slot + row * 32 + ((2 * c) ^ (row & 7)) * 4), b = *(const float4*)(slot + row * 32 + ((2 * c + 1) ^ (row & 7)) * 4);
-  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+// A lane's columns kN c ... of row `row` of the staged chunk.
+template <int kN>
+__device__ __forceinline__ void read_slot(const float* slot, int row, int c, float (&v)[kN]) {
+#pragma unroll
+  for (int k = 0; k < kN; k += 4) {
+    const float4 a = *(const float4*)(slot + row * 32 + ((kN / 4 * c + k / 4) ^ (row & 7)) * 4);
+    v[k] = a.x, v[k + 1] = a.y, v[k + 2] = a.z, v[k + 3] = a.w;
+  }
 }
 
 // y and z of a chunk.  kWhole: all 32 x 32 elements exist, in 16-byte pieces.
 template <typename T, bool kWhole>
 __device__ __forceinline__ void layer_chunk(const ProductGroup& g, int q, int m0, int n0, int exponent, const float* slot) {
-  const int lane = threadIdx.x % 32, c = lane % 4, n = n0 + 8 * c, row = lane / 4, count = kWhole ? 8 : min(8, g.N - n), rows = kWhole ? 32 : g.M - m0 - row;
-  float bias[8];
+  constexpr int kN = sizeof(T) == 4 ? 4 : 8, kLanes = 32 / kN;
+  const int lane = threadIdx.x % 32, c = lane % kLanes, n = n0 + kN * c, row = lane / kLanes, count = kWhole ? kN : min(kN, g.N - n), rows = kWhole ? 32 : g.M - m0 - row;
+  float bias[kN];
   if (g.bias) {
     const T* b = (const T*)g.bias + q * g.bias_batch + n;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) bias[k] = kWhole || k < count ? (float)b[k] : 0.0f;
+    for (int k = 0; k < kN; ++k) bias[k] = kWhole || k < count ? (float)b[k] : 0.0f;
   }
   // 2^exponent as two factors, so that neither leaves fp32's range
   const float f0 = ldexpf(1.0f, exponent / 2), f1 = ldexpf(1.0f, exponent - exponent / 2);
@@ -405,66 +444,80 @@ __device__ __forceinline__ void layer_chunk(const ProductGroup& g, int q, int m0
   T* z = (T*)g.z + q * g.z_batch + (int64_t)(m0 + row) * g.z_row + n;
   T* y = (T*)g.out + q * g.out_batch + (int64_t)(m0 + row) * g.out_row + n;
 #pragma unroll kWhole ? 4 : 1
-  for (int i = 0; i < 4; ++i, r += 8 * g.residual_row, z += 8 * g.z_row, y += 8 * g.out_row) {
-    if (!kWhole && (8 * i >= rows || count <= 0)) break;
-    float v[8], add[8];
-    if (g.residual) load8<T, kWhole>(r, count, add);
-    read_slot(slot, 8 * i + row, c, v);
+  for (int i = 0; i < 32 / kN; ++i, r += kN * g.residual_row, z += kN * g.z_row, y += kN * g.out_row) {
+    if (!kWhole && (kN * i >= rows || count <= 0)) break;
+    float v[kN], add[kN];
+    if (g.residual) load_values<T, kWhole>(r, count, add);
+    read_slot(slot, kN * i + row, c, v);
     if (sizeof(T) == 4) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = v[k] * f0 * f1;
+      for (int k = 0; k < kN; ++k) v[k] = v[k] * f0 * f1;
     }
     if (g.bias) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] += bias[k];
+      for (int k = 0; k < kN; ++k) v[k] += bias[k];
     }
-    if (g.z) store8<T, kWhole>(z, count, v);
-    activate8(v, g.activation);
+    if (g.z) store_values<T, kWhole>(z, count, v);
+    activate_all(v, g.activation);
     if (g.residual) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] += add[k];
+      for (int k = 0; k < kN; ++k) v[k] += add[k];
     }
-    store8<T, kWhole>(y, count, v);
+    store_values<T, kWhole>(y, count, v);
   }
 }
 
 // The local step and the pull of a chunk of a worker's matrix.
-template <typename T>
-__device__ __forceinline__ void step_chunk(const ProductParams& p, const ProductGroup& g, int q, int m0, int n0, const float* slot, const Residual& residual) {
-  const int lane = threadIdx.x % 32, c = lane % 4, n = n0 + 8 * c, row = lane / 4, count = min(8, g.N - n), rows = count > 0 ? g.M - m0 - row : 0;
+template <typename T, int kN, int kAhead>
+__device__ __forceinline__ void step_chunk(const ProductParams& p, const ProductGroup& g, int q, int m0, int n0, const float* slot) {
+  constexpr int kLanes = 32 / kN;
+  const int lane = threadIdx.x % 32, c = lane % kLanes, n = n0 + kN * c, row = lane / kLanes, count = min(kN, g.N - n), rows = count > 0 ? g.M - m0 - row : 0;
   const PullParams& s = p.step;
   const int matrix = g.first_matrix + q / s.workers, worker = q % s.workers;
   const float scale = p.matrix_scale[matrix] * kPlaneUnscale;
   const int peer = s.peers[worker * s.draw_stride];
   const bool pull = peer != worker && (uint32_t)peer < (uint32_t)s.workers;
   const float w = pull ? s.weights[worker * s.draw_stride] : 0.0f;
-  const int64_t at = (int64_t)p.matrix_offset[matrix] + (int64_t)(m0 + row) * g.out_row + n, step = 8 * g.out_row;
+  const int64_t at = (int64_t)p.matrix_offset[matrix] + (int64_t)(m0 + row) * g.out_row + n, step = kN * g.out_row;
   const T* own = (const T*)s.x + worker * s.x_row + at;
   const T* other = (const T*)s.x + (pull ? peer : worker) * s.x_row + at;
   T* next = (T*)s.x_next + worker * s.next_row + at;
-  const bool whole = count == 8 && (((uintptr_t)own | (uintptr_t)other | (uintptr_t)next | (uintptr_t)(step * sizeof(T))) & 15) == 0;
+  const bool whole = count == kN && (((uintptr_t)own | (uintptr_t)other | (uintptr_t)next | (uintptr_t)(step * sizeof(T))) & 15) == 0;
+  const __half* planes = (const __half*)g.residual + q * g.residual_batch + (int64_t)(m0 + row) * g.residual_row + n;
 #pragma unroll
-  for (int i = 0; i < 4; ++i, own += step, other += step, next += step) {
-    if (8 * i >= rows) break;
-    float xi[8], xm[8], v[8], x[8], lo[8];
-    if (whole) {
-      load8<T, true>(own, 8, xi);
-      load8<T, true>(other, 8, xm);
-    } else {
-      load8<T, false>(own, count, xi);
-      load8<T, false>(other, count, xm);
-    }
-    read_slot(slot, 8 * i + row, c, v);
-    unpack_half(residual.hi[i], x);
-    unpack_half(residual.lo[i], lo);
+  for (int i0 = 0; i0 < 32 / kN; i0 += kAhead) {  // kAhead rows in flight
+    float xi[kAhead][kN], xm[kAhead][kN];
+    uint32_t hi[kAhead][kN / 2], lo[kAhead][kN / 2];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float o = scale * fmaf(p.ca, x[k] + lo[k], v[k] * kPlaneUnscale);
-      const float h = fmaf(-s.lr, fmaf(s.decay, xi[k], o), xi[k]);
-      v[k] = pull ? fmaf(-w, h - xm[k], h) : h;
+    for (int u = 0; u < kAhead; ++u) {
+      if (kN * (i0 + u) >= rows) break;
+      load_words(planes + (i0 + u) * kN * g.residual_row, hi[u]);
+      load_words(planes + (i0 + u) * kN * g.residual_row + g.residual_plane, lo[u]);
+      if (whole) {
+        load_values<T, true>(own + (i0 + u) * step, kN, xi[u]);
+        load_values<T, true>(other + (i0 + u) * step, kN, xm[u]);
+      } else {
+        load_values<T, false>(own + (i0 + u) * step, count, xi[u]);
+        load_values<T, false>(other + (i0 + u) * step, count, xm[u]);
+      }
     }
-    if (whole) store8<T, true>(next, 8, v);
-    else store8<T, false>(next, count, v);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = i0 + u;
+      if (kN * i >= rows) break;
+      float v[kN], x[kN], xl[kN];
+      read_slot(slot, kN * i + row, c, v);
+      unpack_half<kN>(hi[u], x);
+      unpack_half<kN>(lo[u], xl);
+#pragma unroll
+      for (int k = 0; k < kN; ++k) {
+        const float o = scale * fmaf(p.ca, x[k] + xl[k], v[k] * kPlaneUnscale);
+        const float h = fmaf(-s.lr, fmaf(s.decay, xi[u][k], o), xi[u][k]);
+        v[k] = pull ? fmaf(-w, h - xm[u][k], h) : h;
+      }
+      if (whole) store_values<T, true>(next + i * step, kN, v);
+      else store_values<T, false>(next + i * step, count, v);
+    }
   }
 }
 
@@ -472,7 +525,7 @@ __device__ __forceinline__ void step_chunk(const ProductParams& p, const Product
 // over a tile's chunks the code outgrew the instruction cache (the 8 x (4096 x 4096 x 4096) layer with silu: 1715 us).
 template <int kEpilogue, int kPlanes>
 __device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const ProductGroup& g, const Tile& t, int m0, int n0, int exponent, float* slot,
-                                               const Residual& residual) {
+                                               const Residual<lane_columns(kEpilogue)>& residual) {
   const int lane = threadIdx.x % 32;
   __syncwarp();
   if (kEpilogue == kLayerF32 || kEpilogue == kLayerBf16) {
@@ -483,59 +536,60 @@ __device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const Pro
   }
   if (kEpilogue == kStepF32 || kEpilogue == kStepBf16) {
     using T = typename std::conditional<kEpilogue == kStepF32, float, __nv_bfloat16>::type;
-    step_chunk<T>(p, g, t.q, m0, n0, slot, residual);
+    step_chunk<T, lane_columns(kEpilogue), kPlanes == 2 ? 2 : 1>(p, g, t.q, m0, n0, slot);
     return;
   }
-  const int c = lane % 4, n = n0 + 8 * c, row = lane / 4, count = min(8, g.N - n), rows = count > 0 ? g.M - m0 - row : 0;
+  constexpr int kN = lane_columns(kEpilogue), kLanes = 32 / kN;
+  const int c = lane % kLanes, n = n0 + kN * c, row = lane / kLanes, count = min(kN, g.N - n), rows = count > 0 ? g.M - m0 - row : 0;
   if (kEpilogue == kLastF32 || kEpilogue == kLastBf16) {
     using T = typename std::conditional<kEpilogue == kLastF32, float, __nv_bfloat16>::type;
     T* out = (T*)g.out + t.q * g.out_batch + (int64_t)(m0 + row) * g.out_row + n;
 #pragma unroll
-    for (int i = 0; i < 4; ++i, out += 8 * g.out_row) {
-      if (8 * i >= rows) break;
-      float v[8], x[8], lo[8];
-      read_slot(slot, 8 * i + row, c, v);
-      unpack_half(residual.hi[i], x);
-      unpack_half(residual.lo[i], lo);
+    for (int i = 0; i < 32 / kN; ++i, out += kN * g.out_row) {
+      if (kN * i >= rows) break;
+      float v[kN], x[kN], lo[kN];
+      read_slot(slot, kN * i + row, c, v);
+      unpack_half<kN>(residual.hi[i], x);
+      unpack_half<kN>(residual.lo[i], lo);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = kPlaneUnscale * fmaf(p.ca, x[k] + lo[k], v[k] * kPlaneUnscale);
-      if (g.pieces) store8<T, true>(out, 8, v);
-      else store8<T, false>(out, count, v);
+      for (int k = 0; k < kN; ++k) v[k] = kPlaneUnscale * fmaf(p.ca, x[k] + lo[k], v[k] * kPlaneUnscale);
+      if (g.pieces) store_values<T, true>(out, kN, v);
+      else store_values<T, false>(out, count, v);
     }
     return;
   }
-  const bool mirrored = kEpilogue != kUpdate && t.i != t.j;
+  const bool mirrored = kEpilogue != kUpdate && t.j < g.symmetric * t.i;
   __half* out = (__half*)g.out + t.q * g.out_batch + (int64_t)(m0 + row) * g.out_row + n;
 #pragma unroll
   for (int i = 0; i < 4; ++i, out += 8 * g.out_row) {
     if (8 * i >= rows) break;
-    float v[8], x[8], lo[8];
+    float v[kN], x[kN], lo[kN];
     read_slot(slot, 8 * i + row, c, v);
     if (kEpilogue >= kPolynomial) {
-      unpack_half(residual.hi[i], x);
+      unpack_half<kN>(residual.hi[i], x);
       if (kEpilogue == kUpdate || kPlanes == 2) {
-        unpack_half(residual.lo[i], lo);
+        unpack_half<kN>(residual.lo[i], lo);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] += lo[k];
+        for (int k = 0; k < kN; ++k) x[k] += lo[k];
       }
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < kN; ++k) {
       v[k] *= kPlaneUnscale;
       if (kEpilogue == kPolynomial) v[k] = fmaf(p.cc, v[k], p.cb * x[k]);
       if (kEpilogue == kUpdate) v[k] = fmaf(p.ca, x[k], v[k]);
     }
-    uint4 h, l;
-    if (kEpilogue == kUpdate || kPlanes == 2) split8(v, h, l);
-    else h = half8(v), l = make_uint4(0, 0, 0, 0);
-    *(uint4*)out = h;
-    if (kEpilogue == kUpdate || kPlanes == 2) *(uint4*)(out + g.out_plane) = l;
+    uint32_t h[kN / 2], l[kN / 2] = {};
+    if (kEpilogue == kUpdate || kPlanes == 2) split_values<kN>(v, h, l);
+    else pack_half<kN>(v, h);
+    store_words(out, h);
+    if (kEpilogue == kUpdate || kPlanes == 2) store_words(out + g.out_plane, l);
     if (mirrored) {  // both planes of an element in one word
       const int r = 8 * i + row;
-      *(uint4*)(slot + r * 32 + ((2 * c) ^ (r & 7)) * 4) =
-          make_uint4(__byte_perm(h.x, l.x, 0x5410), __byte_perm(h.x, l.x, 0x7632), __byte_perm(h.y, l.y, 0x5410), __byte_perm(h.y, l.y, 0x7632));
-      *(uint4*)(slot + r * 32 + ((2 * c + 1) ^ (r & 7)) * 4) =
-          make_uint4(__byte_perm(h.z, l.z, 0x5410), __byte_perm(h.z, l.z, 0x7632), __byte_perm(h.w, l.w, 0x5410), __byte_perm(h.w, l.w, 0x7632));
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        *(uint4*)(slot + r * 32 + ((2 * c + k) ^ (r & 7)) * 4) = make_uint4(__byte_perm(h[2 * k], l[2 * k], 0x5410), __byte_perm(h[2 * k], l[2 * k], 0x7632),
+                                                                           __byte_perm(h[2 * k + 1], l[2 * k + 1], 0x5410), __byte_perm(h[2 * k + 1], l[2 * k + 1], 0x7632));
     }
   }
   if (!mirrored) return;
@@ -556,15 +610,17 @@ __device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const Pro
 }
 
 // kPlanes = 2 (fp32 operands): every kPromote steps of 64 k the accumulator goes to fp32 registers and starts over.  The tensor cores drop
-// what lies below the running sum's last bit at every 16 k, so the error grows with k (2-norm, K = 2048: 7.4e-6; with the sum taken over
-// every 128 k 1e-6 at any K); the epilogue warps add a part under the products of the next.
-constexpr int kPromote = 2;
+// what lies below the running sum's last bit at every 16 k, so the error grows with k (2-norm, K = 2048: 7.4e-6); with the sum taken over
+// every 256 k it is 8.4e-7 at any K (fp32 FMAs: 4.1e-7 at K = 512, 1.1e-6 at 4096), every 128 k 3.9e-7, but then the products wait for
+// accumulators (four layers of 2048 x 2048 x 2048: 183 us, 172 so, 168 without).
+constexpr int kPromote = 4;
 
 template <int kCtas, int kEpilogue, int kPlanes>
-__global__ __launch_bounds__(product_threads(kPlanes), 1) void product_kernel(const __grid_constant__ ProductParams p) {
-  constexpr int kEpilogueWarps = epilogue_warps(kPlanes), kLoader = kEpilogueWarps, kMultiplier = kEpilogueWarps + 1;
+__global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __grid_constant__ ProductParams p) {
+  constexpr int kLoader = kEpilogueWarps, kMultiplier = kEpilogueWarps + 1;
   extern __shared__ unsigned char raw[];
-  __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 4];
+  constexpr int kAccumulators = accumulators(kPlanes), kAccumulatorColumns = 512 / kAccumulators;
+  __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 2 * kAccumulators];
   __shared__ uint32_t tmem_at;
   __shared__ volatile uint32_t gave_up;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -572,13 +628,13 @@ __global__ __launch_bounds__(product_threads(kPlanes), 1) void product_kernel(co
   // (the same offset in both CTAs of a pair: dynamic shared memory starts at the same address in every CTA)
   const uint32_t base = (ptx::smem(raw) + 1023) & ~1023u;
   float* const slots = (float*)(raw + (base - ptx::smem(raw)) + (size_t)p.stages * p.stage_bytes);
-  const uint32_t full = ptx::smem(bars), empty = full + 8 * kMaxStages, done = empty + 8 * kMaxStages, drained = done + 16;
+  const uint32_t full = ptx::smem(bars), empty = full + 8 * kMaxStages, done = empty + 8 * kMaxStages, drained = done + 8 * kAccumulators;
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       ptx::barrier_init(full + 8 * s, 1);
       ptx::barrier_init(empty + 8 * s, 1);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < kAccumulators; ++b) {
       ptx::barrier_init(done + 8 * b, 1);
       ptx::barrier_init(drained + 8 * b, kEpilogueWarps * kCtas);
     }
@@ -601,9 +657,6 @@ __global__ __launch_bounds__(product_threads(kPlanes), 1) void product_kernel(co
     *(volatile unsigned int*)p.error = 1;
     __threadfence_system();
   };
-  // Two planes: 128 of an epilogue thread's registers are sums.  168 a thread at the launch, 64,512 in all: (2 x 216 + 72) x 128.
-  if (warp >= kEpilogueWarps) {
-  if (kPlanes == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   if (warp == kLoader && ptx::elect()) {  // ---- loads
     int issued = 0;  // stages filled so far
     bool ok = true;
@@ -650,10 +703,10 @@ __global__ __launch_bounds__(product_threads(kPlanes), 1) void product_kernel(co
       const uint32_t step_a = g.a_mn ? 2048 : 32, step_b = g.b_mn ? 2048 : 32;  // 16 k further
       const int steps = (g.K + 63) / 64, per_part = kPlanes == 2 ? kPromote : steps;
       for (int begin = 0; begin < steps && ok; begin += per_part, ++part) {
-        const int acc = part & 1, lap = part >> 1;
+        const int acc = part % kAccumulators, lap = part / kAccumulators;
         if (lap > 0 && !ptx::wait(drained + 8 * acc, (lap - 1) & 1)) { ok = false; break; }
         ptx::fence_after();
-        const uint32_t d = tmem + acc * 256;
+        const uint32_t d = tmem + acc * kAccumulatorColumns;
         for (int kb = begin; kb < min(steps, begin + per_part); ++kb, ++used) {
           const int s = used % p.stages;
           if (!ptx::wait(full + 8 * s, (used / p.stages) & 1) || gave_up) { ok = false; break; }
@@ -672,10 +725,8 @@ __global__ __launch_bounds__(product_threads(kPlanes), 1) void product_kernel(co
       }
     }
     if (!ok) failed();
-  }
-  } else {  // ---- epilogue: warp w has lanes 32 (w % 4) ... of the accumulator and every second (fourth) 32 columns from w / 4 on
-    if (kPlanes == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-    const uint32_t quadrant = warp % 4, half = warp / 4;
+  } else if (warp < kEpilogueWarps) {  // ---- epilogue: warp w has lanes 32 (w % 4) ... of the accumulator and every second (fourth) 32 columns from w / 4 on
+    const uint32_t quadrant = warp % 4, column = warp / 4 * 32;
     float* const slot = slots + warp * (kSlotBytes / 4);
     int part = 0;
     bool ok = true;
@@ -687,42 +738,36 @@ __global__ __launch_bounds__(product_threads(kPlanes), 1) void product_kernel(co
       int exponent = 0;
       if (kEpilogue == kLayerF32) exponent = -(g.exp_a[g.a_batched ? tile.q : 0] + g.exp_b[g.b_batched ? tile.q : 0]);
       const int steps = (g.K + 63) / 64, per_part = kPlanes == 2 ? kPromote : steps;
-      Residual residual;
-      if (kPlanes == 1 && (int)half * 32 < columns) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + (int)half * 32, lane, residual);
-      float sum[kPlanes == 2 ? 4 : 1][32];
+      Residual<lane_columns(kEpilogue)> residual;
+      if ((int)column < columns) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + column, lane, residual);
+      float sum[32];
       if (kPlanes == 2) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-          for (int c = 0; c < 32; ++c) sum[k][c] = 0.0f;
+        for (int c = 0; c < 32; ++c) sum[c] = 0.0f;
       }
       for (int begin = 0; begin < steps; begin += per_part, ++part) {
-        const int acc = part & 1, lap = part >> 1;
+        const int acc = part % kAccumulators, lap = part / kAccumulators;
         if (!__all_sync(0xFFFFFFFFu, ptx::wait(done + 8 * acc, lap & 1))) {
           if (lane == 0) failed();
           ok = false;
           break;
         }
         ptx::fence_after();
-        const uint32_t from = tmem + (quadrant * 32 << 16) + acc * 256;
+        const uint32_t from = tmem + (quadrant * 32 << 16) + acc * kAccumulatorColumns;
         if (kPlanes == 2) {
+          if ((int)column < columns) {
+            float v[32];
+            ptx::tmem_load32(from + column, v);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int c = (int)half * 32 + 64 * k;
-            if (c < columns) {
-              float v[32];
-              ptx::tmem_load32(from + c, v);
-#pragma unroll
-              for (int e = 0; e < 32; ++e) sum[k][e] += v[e];
-            }
+            for (int e = 0; e < 32; ++e) sum[e] += v[e];
           }
         } else {
 #pragma unroll 1
-          for (int c = (int)half * 32; c < columns; c += 8 * kEpilogueWarps) {
-            if (c != (int)half * 32) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + c, lane, residual);
-            ptx::tmem_load32(from + c, sum[0]);
+          for (int c = (int)column; c < columns; c += 128) {
+            if (c != (int)column) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + c, lane, residual);
+            ptx::tmem_load32(from + c, sum);
             __syncwarp();
-            stage_row(slot, sum[0]);
+            stage_row(slot, sum);
             epilogue_chunk<kEpilogue, kPlanes>(p, g, tile, m0, n0 + c, exponent, slot, residual);
           }
         }
@@ -733,19 +778,10 @@ __global__ __launch_bounds__(product_threads(kPlanes), 1) void product_kernel(co
           else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(drained + 8 * acc) : "memory");
         }
       }
-      if (kPlanes == 2 && ok) {
-#pragma unroll 1
-        for (int k = 0; k < 4; ++k) {
-          const int c = (int)half * 32 + 64 * k;
-          if (c >= columns) break;
-          load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + c, lane, residual);
-          __syncwarp();
-          if (k == 0) stage_row(slot, sum[0]);
-          else if (k == 1) stage_row(slot, sum[kPlanes == 2 ? 1 : 0]);
-          else if (k == 2) stage_row(slot, sum[kPlanes == 2 ? 2 : 0]);
-          else stage_row(slot, sum[kPlanes == 2 ? 3 : 0]);
-          epilogue_chunk<kEpilogue, kPlanes>(p, g, tile, m0, n0 + c, exponent, slot, residual);
-        }
+      if (kPlanes == 2 && ok && (int)column < columns) {
+        __syncwarp();
+        stage_row(slot, sum);
+        epilogue_chunk<kEpilogue, kPlanes>(p, g, tile, m0, n0 + column, exponent, slot, residual);
       }
     }
   }

@@ -6,7 +6,9 @@ carried on entrywise in the basis of the singular vectors, by the divided differ
 a = 3.4445.  A step adds at most C u |X|_F itself, C = 40: |X|_2 <= 1.21, |S|_2 <= 1.46 and |P|_2 <= 2.81 bound the parts
 (|b| + 2 |c| |S|) (2 |X| + |S| / |X|) |X| + |P| (1 + |X|) + |X'| of S = X X^T, P = b S + c S^2 and X' = a X + P X, each rounded by u.
 The errors are spread like noise over the directions, so their factors are taken as the root mean square of the divided differences.
-fp32: u = 2^-20 (22-bit factors, and 24 steps between two fp32 sums that each drop less than 2^-24).
+fp32: u = 2^-20 (22-bit factors; 48 steps between two fp32 sums, each of which drops less than 2^-24 of a running sum that is half the
+final one on average and whose terms have both signs: at most 24 2^-24 = 1.5 2^-20 if they had one, and C, which takes every part at its
+largest, has that much room).
 Small matrices (side up to 64 and length up to 512, or 128 and 256) have 22-bit factors with bfloat16 storage as well: u = 2^-20, and the
 result's rounding, 2^-8 of itself.
 bfloat16, larger: the factors' rounding to fp16 is part of the definition (u = 2^-12); the emulation rounds at the same places in 64 bits, and the
