@@ -1,13 +1,14 @@
-// The layer for batches of a few rows (up to kFewRows): bound by reading the weights once, so they go through the FMA units as they
-// are.  A warp takes kOutputs outputs at a time, its lanes share out k, and all rows of the batch use a weight while it is in a register.
-// The tensor cores' path reads fp32 weights twice and writes them as planes first.  us, this / that: four workers' 1 x 512 x 10 fp32
-// layers 12.8 on that path; see the launch's rule for the larger ones.
+// The layer for batches of a few rows: bound by reading the weights once, so they go through the FMA units as they are.  A warp takes
+// kOutputs outputs at a time, its lanes share out k, and all rows of the batch use a weight while it is in a register.  The tensor
+// cores' path reads fp32 weights twice and writes them as planes first.  us for 8 workers' 4096 x 4096 layers, this / that path: fp32 (read
+// in 82) 1 row 82, 4 rows 123, 8 rows 140 / 431, 16 rows in two passes; bfloat16 (41) 1 row 45, 4 rows 66 / 63, 8 rows 117 / 63.
 #pragma once
 #include "netmax_operators.cuh"
 
 namespace netmax {
 
-constexpr int kFewRows = 8;
+// Up to so many rows: fp32; bfloat16 that the tensor cores can read in place; bfloat16 that would have to be laid out first.
+constexpr int kFewRowsF32 = 16, kFewRowsBf16 = 4, kFewRowsBf16Laid = 8;
 
 struct FewRowsParams {
   const void *x = nullptr, *weight = nullptr, *bias = nullptr, *residual = nullptr;
@@ -24,11 +25,12 @@ __global__ __launch_bounds__(kElementThreads) void few_rows_kernel(const __grid_
   constexpr int kN = 16 / sizeof(T);  // values of a load
   ptx::let_successor_start();
   ptx::wait_for_predecessor();
-  if (blockIdx.x + blockIdx.y == 0 && threadIdx.x == 0) *p.error = 0;
+  if (blockIdx.x + blockIdx.y + blockIdx.z == 0 && threadIdx.x == 0) *p.error = 0;
   const int lane = threadIdx.x % 32, first = (blockIdx.x * (kElementThreads / 32) + threadIdx.x / 32) * kOutputs;
   if (first >= p.n_out) return;
   const int64_t q = blockIdx.y;
-  const T* x = (const T*)p.x + q * p.x_batch;
+  const int rows_before = blockIdx.z * kRows, n = min(kRows, p.n - rows_before);
+  const T* x = (const T*)p.x + q * p.x_batch + rows_before * p.x_row;
   const T* w = (const T*)p.weight + q * p.weight_batch + first * p.weight_row;
   float sum[kOutputs][kRows] = {};
   auto step = [&](int k, int count, auto whole) {
@@ -43,7 +45,7 @@ __global__ __launch_bounds__(kElementThreads) void few_rows_kernel(const __grid_
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
       float b[kN];
-      load_values<T, kWhole, kN>(x + (r < p.n ? r : p.n - 1) * p.x_row + k, count, b);
+      load_values<T, kWhole, kN>(x + (r < n ? r : n - 1) * p.x_row + k, count, b);
 #pragma unroll
       for (int o = 0; o < kOutputs; ++o)
 #pragma unroll
@@ -66,8 +68,9 @@ __global__ __launch_bounds__(kElementThreads) void few_rows_kernel(const __grid_
       for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
       if (lane == o * kRows + r) mine = s;
     }
-  const int o = first + lane / kRows, r = lane % kRows;
-  if (lane >= kOutputs * kRows || o >= p.n_out || r >= p.n) return;
+  const int o = first + lane / kRows;
+  if (lane >= kOutputs * kRows || o >= p.n_out || lane % kRows >= n) return;
+  const int64_t r = rows_before + lane % kRows;
   if (p.bias) mine += (float)((const T*)p.bias)[q * p.bias_batch + o];
   if (p.z) ((T*)p.z)[q * p.z_batch + r * p.z_row + o] = (T)mine;
   mine = activate(mine, p.activation);

@@ -433,24 +433,26 @@ int few_rows(Stream& s, const netmax_layer& l) {
   };
   p.pieces = fits(l.x, l.n) && fits(l.weight, l.n_out);
   const int rows = l.n <= 1 ? 1 : l.n <= 2 ? 2 : l.n <= 4 ? 4 : 8;
-  // two outputs a warp share the loads of x; one where that would leave SMs without work
-  const bool two = l.M * ceil_div<int64_t>(l.n_out, 16) >= sm_count();
-  const dim3 grid((unsigned)ceil_div<int64_t>(l.n_out, two ? 16 : 8), (unsigned)l.M);
-  auto run = [&](void (*kernel)(const FewRowsParams)) { return launch(s, kernel, grid, kElementThreads, 0, 1, p); };
+  // several outputs a warp share the loads of x; one where that would leave SMs without work
+  const int most = rows >= 4 ? 4 : 2, outputs = l.M * ceil_div<int64_t>(l.n_out, 8 * most) >= sm_count() ? most : 1;
+  const dim3 grid((unsigned)ceil_div<int64_t>(l.n_out, 8 * outputs), (unsigned)l.M, (unsigned)ceil_div<int64_t>(l.n, rows));
+  auto run = [&](void (*several)(const FewRowsParams), void (*one)(const FewRowsParams)) {
+    return launch(s, outputs > 1 ? several : one, grid, kElementThreads, 0, 1, p);
+  };
   if (f32) {
     switch (rows) {
-      case 1: return run(two ? few_rows_kernel<float, 1, 2> : few_rows_kernel<float, 1, 1>);
-      case 2: return run(two ? few_rows_kernel<float, 2, 2> : few_rows_kernel<float, 2, 1>);
-      case 4: return run(two ? few_rows_kernel<float, 4, 2> : few_rows_kernel<float, 4, 1>);
-      default: return run(two ? few_rows_kernel<float, 8, 2> : few_rows_kernel<float, 8, 1>);
+      case 1: return run(few_rows_kernel<float, 1, 2>, few_rows_kernel<float, 1, 1>);
+      case 2: return run(few_rows_kernel<float, 2, 2>, few_rows_kernel<float, 2, 1>);
+      case 4: return run(few_rows_kernel<float, 4, 4>, few_rows_kernel<float, 4, 1>);
+      default: return run(few_rows_kernel<float, 8, 4>, few_rows_kernel<float, 8, 1>);
     }
   }
   using B = __nv_bfloat16;
   switch (rows) {
-    case 1: return run(two ? few_rows_kernel<B, 1, 2> : few_rows_kernel<B, 1, 1>);
-    case 2: return run(two ? few_rows_kernel<B, 2, 2> : few_rows_kernel<B, 2, 1>);
-    case 4: return run(two ? few_rows_kernel<B, 4, 2> : few_rows_kernel<B, 4, 1>);
-    default: return run(two ? few_rows_kernel<B, 8, 2> : few_rows_kernel<B, 8, 1>);
+    case 1: return run(few_rows_kernel<B, 1, 2>, few_rows_kernel<B, 1, 1>);
+    case 2: return run(few_rows_kernel<B, 2, 2>, few_rows_kernel<B, 2, 1>);
+    case 4: return run(few_rows_kernel<B, 4, 4>, few_rows_kernel<B, 4, 1>);
+    default: return run(few_rows_kernel<B, 8, 4>, few_rows_kernel<B, 8, 1>);
   }
 }
 
@@ -587,7 +589,8 @@ int netmax_layer_forward(const netmax_layer* l) try {
     OP_CUDA(cudaMemsetAsync(l->workspace, 0, 4, s.stream));
     return NETMAX_OK;
   }
-  if (n <= kFewRows) return few_rows(s, *l);
+  const bool f32 = l->storage == NETMAX_STORAGE_F32;
+  if (n <= (f32 ? kFewRowsF32 : aligned16(l->weight, l->M) ? kFewRowsBf16 : kFewRowsBf16Laid)) return few_rows(s, *l);
   OperandParams jobs;
   int n_jobs = 0;
   const Prepared w = prepare_operand(l->weight, nullptr, 0, l->M, n_out, n_in, l->storage, room.weight, jobs, n_jobs);

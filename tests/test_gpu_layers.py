@@ -63,6 +63,7 @@ def check(got, want, bound, what):
 SIZES = [  # M, n, n_in, n_out
     (1, 1, 1, 1), (2, 1, 5, 3), (4, 1, 512, 10), (3, 7, 64, 64), (2, 64, 64, 128), (1, 130, 129, 131), (5, 77, 1001, 333), (2, 300, 72, 520),
     (1, 2, 4100, 17), (2, 513, 8, 264), (1, 1024, 768, 1280), (3, 2, 16, 2050), (37, 3, 24, 40),
+    (2, 11, 520, 1300), (3, 16, 130, 77), (150, 8, 40, 33), (160, 4, 72, 48), (2, 5, 1001, 600), (1, 9, 64, 5000),
 ]
 
 
