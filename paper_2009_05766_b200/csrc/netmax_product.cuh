@@ -441,36 +441,47 @@ __device__ __forceinline__ void read_slot(const float* slot, int row, int c, flo
   }
 }
 
+// What a chunk's function reads of its group over and over, once in registers: read in place, every use is an indexed load from the
+// constant bank that the stores in between make the compiler repeat (a ragged chunk took 5 us so).
+struct LayerRows {
+  int64_t out, z, residual;
+  bool has_z, has_residual, has_bias;
+  int activation;
+  __device__ __forceinline__ explicit LayerRows(const ProductGroup& g)
+      : out(g.out_row), z(g.z_row), residual(g.residual_row), has_z(g.z != nullptr), has_residual(g.residual != nullptr), has_bias(g.bias != nullptr),
+        activation(g.activation) {}
+};
 // y and z of a chunk whose 32 x 32 elements all exist, in 16-byte pieces.
 template <typename T>
 __device__ __forceinline__ void layer_chunk(const ProductGroup& g, int q, int m0, int n0, float f0, float f1, const float* slot) {
   constexpr int kN = sizeof(T) == 4 ? 4 : 8, kLanes = 32 / kN;
   const int lane = threadIdx.x % 32, c = lane % kLanes, n = n0 + kN * c, row = lane / kLanes;
+  const LayerRows g1(g);
   float bias[kN];
-  if (g.bias) {
+  if (g1.has_bias) {
     const T* b = (const T*)g.bias + q * g.bias_batch + n;
 #pragma unroll
     for (int k = 0; k < kN; ++k) bias[k] = (float)b[k];
   }
-  const T* r = (const T*)g.residual + q * g.residual_batch + (int64_t)(m0 + row) * g.residual_row + n;
-  T* z = (T*)g.z + q * g.z_batch + (int64_t)(m0 + row) * g.z_row + n;
-  T* y = (T*)g.out + q * g.out_batch + (int64_t)(m0 + row) * g.out_row + n;
+  const T* r = (const T*)g.residual + q * g.residual_batch + (int64_t)(m0 + row) * g1.residual + n;
+  T* z = (T*)g.z + q * g.z_batch + (int64_t)(m0 + row) * g1.z + n;
+  T* y = (T*)g.out + q * g.out_batch + (int64_t)(m0 + row) * g1.out + n;
 #pragma unroll
-  for (int i = 0; i < 32 / kN; ++i, r += kN * g.residual_row, z += kN * g.z_row, y += kN * g.out_row) {
+  for (int i = 0; i < 32 / kN; ++i, r += kN * g1.residual, z += kN * g1.z, y += kN * g1.out) {
     float v[kN], add[kN];
-    if (g.residual) load_values<T, true>(r, kN, add);
+    if (g1.has_residual) load_values<T, true>(r, kN, add);
     read_slot(slot, kN * i + row, c, v);
     if (sizeof(T) == 4) {
 #pragma unroll
       for (int k = 0; k < kN; ++k) v[k] = v[k] * f0 * f1;
     }
-    if (g.bias) {
+    if (g1.has_bias) {
 #pragma unroll
       for (int k = 0; k < kN; ++k) v[k] += bias[k];
     }
-    if (g.z) store_values<T, true>(z, kN, v);
-    activate_all(v, g.activation);
-    if (g.residual) {
+    if (g1.has_z) store_values<T, true>(z, kN, v);
+    activate_all(v, g1.activation);
+    if (g1.has_residual) {
 #pragma unroll
       for (int k = 0; k < kN; ++k) v[k] += add[k];
     }
@@ -480,31 +491,39 @@ __device__ __forceinline__ void layer_chunk(const ProductGroup& g, int q, int m0
 // Of any chunk: a column a lane, so that a row's elements still go out together whatever their alignment.
 template <typename T>
 __device__ __forceinline__ void ragged_layer_chunk(const ProductGroup& g, int q, int m0, int n0, float f0, float f1, const float* slot) {
-  const int lane = threadIdx.x % 32, n = n0 + lane, rows = min(32, g.M - m0);
-  if (n >= g.N) return;
-  const float bias = g.bias ? (float)((const T*)g.bias)[q * g.bias_batch + n] : 0.0f;
-  const T* r = (const T*)g.residual + q * g.residual_batch + (int64_t)m0 * g.residual_row + n;
-  T* z = (T*)g.z + q * g.z_batch + (int64_t)m0 * g.z_row + n;
-  T* y = (T*)g.out + q * g.out_batch + (int64_t)m0 * g.out_row + n;
+  const int lane = threadIdx.x % 32, n = n0 + lane, rows = n < g.N ? min(32, g.M - m0) : 0;
+  const LayerRows g1(g);
+  const float bias = g1.has_bias && rows > 0 ? (float)((const T*)g.bias)[q * g.bias_batch + n] : 0.0f;
+  const T* r = (const T*)g.residual + q * g.residual_batch + (int64_t)m0 * g1.residual + n;
+  T* z = (T*)g.z + q * g.z_batch + (int64_t)m0 * g1.z + n;
+  T* y = (T*)g.out + q * g.out_batch + (int64_t)m0 * g1.out + n;
 #pragma unroll 1
-  for (int i0 = 0; i0 < rows; i0 += 8) {
+  for (int i0 = 0; i0 < 32; i0 += 8, r += 8 * g1.residual, z += 8 * g1.z, y += 8 * g1.out) {
     float v[8], add[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const int i = i0 + u;
       v[u] = slot[i * 32 + ((lane / 4) ^ (i & 7)) * 4 + lane % 4];
-      add[u] = g.residual && i < rows ? (float)r[i * g.residual_row] : 0.0f;
       if (sizeof(T) == 4) v[u] = v[u] * f0 * f1;
-      if (g.bias) v[u] += bias;
-      if (g.z && i < rows) z[i * g.z_row] = (T)v[u];
+      v[u] += bias;
     }
-    activate_all(v, g.activation);
+    if (g1.has_residual) {
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int i = i0 + u;
-      if (g.residual) v[u] += add[u];
-      if (i < rows) y[i * g.out_row] = (T)v[u];
+      for (int u = 0; u < 8; ++u) add[u] = i0 + u < rows ? (float)r[u * g1.residual] : 0.0f;
     }
+    if (g1.has_z) {
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (i0 + u < rows) z[u * g1.z] = (T)v[u];
+    }
+    activate_all(v, g1.activation);
+    if (g1.has_residual) {
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] += add[u];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (i0 + u < rows) y[u * g1.out] = (T)v[u];
   }
 }
 
@@ -524,6 +543,8 @@ __device__ __forceinline__ void step_chunk(const ProductParams& p, const Product
   const T* other = (const T*)s.x + (pull ? peer : worker) * s.x_row + at;
   T* next = (T*)s.x_next + worker * s.next_row + at;
   const bool whole = count == kN && (((uintptr_t)own | (uintptr_t)other | (uintptr_t)next | (uintptr_t)(step * sizeof(T))) & 15) == 0;
+  const int64_t plane = g.residual_plane, plane_step = kN * g.residual_row;
+  const float ca = p.ca, lr = s.lr, decay = s.decay;
   const __half* planes = (const __half*)g.residual + q * g.residual_batch + (int64_t)(m0 + row) * g.residual_row + n;
 #pragma unroll
   for (int i0 = 0; i0 < 32 / kN; i0 += kAhead) {  // kAhead rows in flight
@@ -532,8 +553,8 @@ __device__ __forceinline__ void step_chunk(const ProductParams& p, const Product
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (kN * (i0 + u) >= rows) break;
-      load_words(planes + (i0 + u) * kN * g.residual_row, hi[u]);
-      load_words(planes + (i0 + u) * kN * g.residual_row + g.residual_plane, lo[u]);
+      load_words(planes + (i0 + u) * plane_step, hi[u]);
+      load_words(planes + (i0 + u) * plane_step + plane, lo[u]);
       if (whole) {
         load_values<T, true>(own + (i0 + u) * step, kN, xi[u]);
         load_values<T, true>(other + (i0 + u) * step, kN, xm[u]);
@@ -552,8 +573,8 @@ __device__ __forceinline__ void step_chunk(const ProductParams& p, const Product
       unpack_half<kN>(lo[u], xl);
 #pragma unroll
       for (int k = 0; k < kN; ++k) {
-        const float o = scale * fmaf(p.ca, x[k] + xl[k], v[k] * kPlaneUnscale);
-        const float h = fmaf(-s.lr, fmaf(s.decay, xi[u][k], o), xi[u][k]);
+        const float o = scale * fmaf(ca, x[k] + xl[k], v[k] * kPlaneUnscale);
+        const float h = fmaf(-lr, fmaf(decay, xi[u][k], o), xi[u][k]);
         v[k] = pull ? fmaf(-w, h - xm[u][k], h) : h;
       }
       if (whole) store_values<T, true>(next + i * step, kN, v);
@@ -584,19 +605,22 @@ __device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const Pro
   }
   constexpr int kN = lane_columns(kEpilogue), kLanes = 32 / kN;
   const int c = lane % kLanes, n = n0 + kN * c, row = lane / kLanes, count = min(kN, g.N - n), rows = count > 0 ? g.M - m0 - row : 0;
+  const int64_t out_step = kN * g.out_row, out_plane = g.out_plane;  // (in registers: see LayerRows)
+  const float ca = p.ca, cb = p.cb, cc = p.cc;
   if (kEpilogue == kLastF32 || kEpilogue == kLastBf16) {
     using T = typename std::conditional<kEpilogue == kLastF32, float, __nv_bfloat16>::type;
     T* out = (T*)g.out + t.q * g.out_batch + (int64_t)(m0 + row) * g.out_row + n;
+    const bool pieces = g.pieces;
 #pragma unroll
-    for (int i = 0; i < 32 / kN; ++i, out += kN * g.out_row) {
+    for (int i = 0; i < 32 / kN; ++i, out += out_step) {
       if (kN * i >= rows) break;
       float v[kN], x[kN], lo[kN];
       read_slot(slot, kN * i + row, c, v);
       unpack_half<kN>(residual.hi[i], x);
       unpack_half<kN>(residual.lo[i], lo);
 #pragma unroll
-      for (int k = 0; k < kN; ++k) v[k] = kPlaneUnscale * fmaf(p.ca, x[k] + lo[k], v[k] * kPlaneUnscale);
-      if (g.pieces) store_values<T, true>(out, kN, v);
+      for (int k = 0; k < kN; ++k) v[k] = kPlaneUnscale * fmaf(ca, x[k] + lo[k], v[k] * kPlaneUnscale);
+      if (pieces) store_values<T, true>(out, kN, v);
       else store_values<T, false>(out, count, v);
     }
     return;
@@ -604,7 +628,7 @@ __device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const Pro
   const bool mirrored = kEpilogue != kUpdate && t.j < g.symmetric * t.i;
   __half* out = (__half*)g.out + t.q * g.out_batch + (int64_t)(m0 + row) * g.out_row + n;
 #pragma unroll
-  for (int i = 0; i < 4; ++i, out += 8 * g.out_row) {
+  for (int i = 0; i < 4; ++i, out += out_step) {
     if (8 * i >= rows) break;
     float v[kN], x[kN], lo[kN];
     read_slot(slot, 8 * i + row, c, v);
@@ -619,14 +643,14 @@ __device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const Pro
 #pragma unroll
     for (int k = 0; k < kN; ++k) {
       v[k] *= kPlaneUnscale;
-      if (kEpilogue == kPolynomial) v[k] = fmaf(p.cc, v[k], p.cb * x[k]);
-      if (kEpilogue == kUpdate) v[k] = fmaf(p.ca, x[k], v[k]);
+      if (kEpilogue == kPolynomial) v[k] = fmaf(cc, v[k], cb * x[k]);
+      if (kEpilogue == kUpdate) v[k] = fmaf(ca, x[k], v[k]);
     }
     uint32_t h[kN / 2], l[kN / 2] = {};
     if (kEpilogue == kUpdate || kPlanes == 2) split_values<kN>(v, h, l);
     else pack_half<kN>(v, h);
     store_words(out, h);
-    if (kEpilogue == kUpdate || kPlanes == 2) store_words(out + g.out_plane, l);
+    if (kEpilogue == kUpdate || kPlanes == 2) store_words(out + out_plane, l);
     if (mirrored) {  // both planes of an element in one word
       const int r = 8 * i + row;
 #pragma unroll
@@ -637,18 +661,18 @@ __device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const Pro
   }
   if (!mirrored) return;
   __syncwarp();  // rows n0 + ..., columns m0 + ...
-  const int m = m0 + 8 * c;
+  const int m = m0 + 8 * c, all_columns = g.N, all_rows = g.M;
   out = (__half*)g.out + t.q * g.out_batch + (int64_t)(n0 + row) * g.out_row + m;
 #pragma unroll
-  for (int i = 0; i < 4; ++i, out += 8 * g.out_row) {
+  for (int i = 0; i < 4; ++i, out += out_step) {
     const int column = 8 * i + row;
     uint32_t w[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(slot[(8 * c + k) * 32 + ((column / 4) ^ k) * 4 + column % 4]);
-    if (n0 + column >= g.N || m >= g.M) continue;
+    if (n0 + column >= all_columns || m >= all_rows) continue;
     *(uint4*)out = make_uint4(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[4], w[5], 0x5410), __byte_perm(w[6], w[7], 0x5410));
     if (kPlanes == 2)
-      *(uint4*)(out + g.out_plane) = make_uint4(__byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632), __byte_perm(w[4], w[5], 0x7632), __byte_perm(w[6], w[7], 0x7632));
+      *(uint4*)(out + out_plane) = make_uint4(__byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632), __byte_perm(w[4], w[5], 0x7632), __byte_perm(w[6], w[7], 0x7632));
   }
 }
 

@@ -175,19 +175,24 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
   const uint32_t parts = (length + 127) / 128;
   bool ok = true;
   uint32_t phase = 0;
-  auto products_done = [&] {  // for all threads alike
-    ok = __syncthreads_and(ptx::wait(ptx::smem(&bar), phase & 1)) != 0;
+  auto products_done = [&] {  // (a thread that gave up once waits no more; all go through the same barriers whatever happens)
+    ok = ok && ptx::wait(ptx::smem(&bar), phase & 1);
     ++phase;
     ptx::fence_after();
   };
-  auto written = [&] {  // what threads have stored is there for the tensor cores
+  // What threads have stored is there for the tensor cores.  With 64 rows the warps of the accumulator's upper half have no more to do.
+  const int busy = side == 64 ? kSmallThreads / 2 : kSmallThreads;
+  auto written = [&] {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     ptx::fence_before();
-    __syncthreads();
+    asm volatile("bar.sync 1, %0;" ::"r"(busy) : "memory");
     ptx::fence_after();
   };
-  written();
-  for (int step = 0; step < p.steps && ok; ++step) {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  ptx::fence_before();
+  __syncthreads();
+  ptx::fence_after();
+  for (int step = 0; step < p.steps && live; ++step) {
     const bool last = step + 1 == p.steps;
     if (warp == 0 && ptx::elect()) {  // S = X X^T
       for (uint32_t part = 0; part < parts; ++part)
@@ -202,8 +207,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
     }
     __syncwarp();
     products_done();
-    if (!ok) break;
-    if (live)
+    {
       for (uint32_t c = (warp / 4) * 16; c < side; c += 64) {
         float v[16], w[16];
         tmem_load16(from + c, v);
@@ -223,6 +227,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
           *(uint4*)(s + s_plane + small_at(side, m, c + 8 * h)) = lo;
         }
       }
+    }
     written();
     if (warp == 0 && ptx::elect()) {  // S S
       for (int term = 0; term < 3; ++term) {
@@ -236,8 +241,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
     }
     __syncwarp();
     products_done();
-    if (!ok) break;
-    if (live)
+    {
       for (uint32_t c = (warp / 4) * 16; c < side; c += 64) {  // P = b S + c S S in S's place: every thread reads what it writes
         float v[16];
         tmem_load16(from + c, v);
@@ -256,6 +260,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
           *at_lo = lo;
         }
       }
+    }
     written();
     if (warp == 0 && ptx::elect()) {  // P X
       for (uint32_t n = 0; n < length; n += 256) {
@@ -271,8 +276,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
     }
     __syncwarp();
     products_done();
-    if (!ok) break;
-    if (live)
+    {
       for (uint32_t c = (warp / 4) * 16; c < length; c += 64) {
         float v[16];
         tmem_load16(from + c, v);
@@ -342,9 +346,10 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
           }
         }
       }
+    }
     written();
   }
-  if (!ok && threadIdx.x == 0) {
+  if (!ok) {
     *(volatile unsigned int*)p.error = 1;
     __threadfence_system();
   }
