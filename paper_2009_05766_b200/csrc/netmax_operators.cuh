@@ -114,7 +114,7 @@ __global__ __launch_bounds__(kElementThreads) void operand_maxima_kernel(const _
   ptx::let_successor_start();
   ptx::wait_for_predecessor();
   if (p.clear_error && blockIdx.x + blockIdx.y + blockIdx.z == 0 && threadIdx.x == 0) *p.error = 0;
-  const OperandJob& j = p.job[blockIdx.z];
+  const OperandJob j = p.job[blockIdx.z];  // (a copy: read in place, its fields are indexed loads from the constant bank, over and over)
   const int blocks = j.sweep.col_tiles * j.sweep.row_blocks;
   if ((int)blockIdx.x >= blocks) return;
   const SweepAt a = sweep_at(j.sweep, blockIdx.x);
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(kElementThreads) void operand_kernel(const __grid_c
   ptx::let_successor_start();
   ptx::wait_for_predecessor();
   if (p.clear_error && blockIdx.x + blockIdx.y + blockIdx.z == 0 && threadIdx.x == 0) *p.error = 0;
-  const OperandJob& j = p.job[blockIdx.z];
+  const OperandJob j = p.job[blockIdx.z];
   const int blocks = j.sweep.col_tiles * j.sweep.row_blocks;
   if ((int)blockIdx.x >= blocks || (sizeof(T) == 4 && !j.dst)) return;
   const SweepAt a = sweep_at(j.sweep, blockIdx.x);
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(kElementThreads) void step_first_iterate_kernel(con
   ptx::wait_for_predecessor();
   const StepSegment seg = p.segment[find_segment(p, blockIdx.x)];
   if (seg.matrix < 0) return;
-  const StepMatrix& to = tables.matrix[seg.matrix];
+  const StepMatrix to = tables.matrix[seg.matrix];
   const Piece piece = piece_of(seg, blockIdx.x);
   const uint32_t pieces = ((seg.offset & 7) + seg.length + kPiece - 1) / kPiece, cols = to.cols;
   const bool whole = ((seg.offset | cols) & 3) == 0;  // groups of four do not cross rows

@@ -210,12 +210,12 @@ __device__ __forceinline__ void cluster_sync() {
 }
 __device__ __forceinline__ void wait_for_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_successor_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-// Shared-memory descriptor of an operand tile in 128-byte swizzled rows.  k contiguous: groups of eight rows are 1024 bytes apart.
-// m (n) contiguous: a row is 64 values of one k; groups of eight k are 1024 bytes apart, blocks of 64 m a box apart.
-__device__ __forceinline__ uint64_t descriptor(uint32_t at, bool mn) {
-  const uint64_t leading = mn ? kBoxBytes >> 4 : 1;
-  return (uint64_t)((at & 0x3FFFF) >> 4) | leading << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
+// Shared-memory descriptor of an operand tile in 128-byte swizzled rows: the low word holds the address and the leading offset, both in
+// 16 bytes, so a place further on is a sum of low words.  k contiguous: groups of eight rows are 1024 bytes apart.  m (n) contiguous: a
+// row is 64 values of one k; groups of eight k are 1024 bytes apart, blocks of 64 m `leading` bytes.
+constexpr uint32_t kDescriptorHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t descriptor_low(uint32_t at, uint32_t leading) { return (at & 0x3FFFF) >> 4 | (leading >> 4) << 16; }
+__device__ __forceinline__ uint64_t descriptor(uint32_t low) { return (uint64_t)kDescriptorHigh << 32 | low; }
 }  // namespace ptx
 
 // Phi(z) and exp(-z^2 / 2) by formula 7.1.26 of Abramowitz and Stegun's handbook, within 1.5e-7: one exponential and one reciprocal for both
@@ -767,7 +767,10 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
     for (int t = first; t < p.tiles && ok; t += stride) {
       const Tile tile = find_tile(p, t);
       const ProductGroup& g = p.group[tile.g];
-      const uint32_t step_a = g.a_mn ? 2048 : 32, step_b = g.b_mn ? 2048 : 32;  // 16 k further
+      // (in 16 bytes, all worked out here: one thread issues, and a product of 256 x 128 x 16 takes 64 cycles)
+      const uint32_t step_a = (g.a_mn ? 2048 : 32) >> 4, step_b = (g.b_mn ? 2048 : 32) >> 4;  // 16 k further
+      const uint32_t low_a = ptx::descriptor_low(base, g.a_mn ? kBoxBytes : 16), low_b = ptx::descriptor_low(base + kPlanes * p.a_bytes, g.b_mn ? kBoxBytes : 16);
+      const uint32_t plane_a = p.a_bytes >> 4, plane_b = p.b_bytes >> 4, stage_step = p.stage_bytes >> 4, idesc = g.idesc;
       const int steps = (g.K + 63) / 64, per_part = kPlanes == 2 ? kPromote : steps;
       for (int begin = 0; begin < steps && ok; begin += per_part, ++part) {
         const int acc = part % kAccumulators, lap = part / kAccumulators;
@@ -778,13 +781,13 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
           const int s = used % p.stages;
           if (!ptx::wait(full + 8 * s, (used / p.stages) & 1) || gave_up) { ok = false; break; }
           ptx::fence_after();
-          const uint32_t at = base + s * p.stage_bytes;
+          const uint32_t at = s * stage_step;
 #pragma unroll
           for (int term = 0; term < (kPlanes == 2 ? 3 : 1); ++term) {  // hi lo, lo hi, hi hi: the small ones first
-            const uint32_t a = at + (kPlanes == 2 && term == 1 ? p.a_bytes : 0), b = at + kPlanes * p.a_bytes + (kPlanes == 2 && term == 0 ? p.b_bytes : 0);
+            const uint32_t a = low_a + at + (kPlanes == 2 && term == 1 ? plane_a : 0), b = low_b + at + (kPlanes == 2 && term == 0 ? plane_b : 0);
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              ptx::mma<kCtas>(d, ptx::descriptor(a + k * step_a, g.a_mn), ptx::descriptor(b + k * step_b, g.b_mn), g.idesc, kb > begin || term + k > 0);
+              ptx::mma<kCtas>(d, ptx::descriptor(a + k * step_a), ptx::descriptor(b + k * step_b), idesc, kb > begin || term + k > 0);
           }
           ptx::commit<kCtas>(empty + 8 * s);
         }

@@ -72,9 +72,6 @@ __device__ __forceinline__ void tmem_load16(uint32_t at, float (&v)[16]) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ uint64_t small_descriptor(uint32_t at, uint32_t leading) {
-  return (uint64_t)((at & 0x3FFFF) >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
 // Byte of element (row, column) in a plane of `side` rows.
 __device__ __forceinline__ uint32_t small_at(uint32_t side, uint32_t row, uint32_t col) {
   return (col / 64) * side * 128 + row * 128 + ((((col % 64) / 8) ^ (row & 7)) * 16) + (col % 8) * 2;
@@ -173,6 +170,9 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
   const uint32_t from = tmem + ((warp % 4) * 32 << 16);
   const bool live = (warp % 4) * 32 < (int)side;
   const uint32_t parts = (length + 127) / 128;
+  // descriptors' low words: X and S k-contiguous, X n-contiguous; offsets in 16 bytes
+  const uint32_t low_x = ptx::descriptor_low(ptx::smem(x), 16), low_s = ptx::descriptor_low(ptx::smem(s), 16), low_xn = ptx::descriptor_low(ptx::smem(x), side * 128);
+  const uint32_t block = side * 8, plane_x = x_plane >> 4, plane_s = s_plane >> 4;
   bool ok = true;
   uint32_t phase = 0;
   auto products_done = [&] {  // (a thread that gave up once waits no more; all go through the same barriers whatever happens)
@@ -195,14 +195,16 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
   for (int step = 0; step < p.steps && live; ++step) {
     const bool last = step + 1 == p.steps;
     if (warp == 0 && ptx::elect()) {  // S = X X^T
-      for (uint32_t part = 0; part < parts; ++part)
+      for (uint32_t part = 0; part < parts; ++part) {
+        const uint32_t d = tmem + part * side, i = idesc | side / 8 << 17, blocks = min(2u, (length - part * 128) / 64);
+#pragma unroll
         for (int term = 0; term < 3; ++term) {
-          const uint32_t a = ptx::smem(x) + (term == 1 ? x_plane : 0), b = ptx::smem(x) + (term == 0 ? x_plane : 0);
-          for (uint32_t k = part * 128; k < min(length, part * 128 + 128); k += 16) {
-            const uint32_t at = (k / 64) * side * 128 + (k % 64) * 2;
-            ptx::mma<1>(tmem + part * side, small_descriptor(a + at, 16), small_descriptor(b + at, 16), idesc | side / 8 << 17, term > 0 || k > part * 128);
-          }
+          uint32_t a = low_x + (term == 1 ? plane_x : 0) + part * 2 * block, b = low_x + (term == 0 ? plane_x : 0) + part * 2 * block;
+          for (uint32_t k = 0; k < blocks; ++k, a += block, b += block)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) ptx::mma<1>(d, ptx::descriptor(a + 2 * u), ptx::descriptor(b + 2 * u), i, term + u > 0 || k > 0);
         }
+      }
       ptx::commit<1>(ptx::smem(&bar));
     }
     __syncwarp();
@@ -230,12 +232,13 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
     }
     written();
     if (warp == 0 && ptx::elect()) {  // S S
+      const uint32_t i = idesc | side / 8 << 17;
+#pragma unroll
       for (int term = 0; term < 3; ++term) {
-        const uint32_t a = ptx::smem(s) + (term == 1 ? s_plane : 0), b = ptx::smem(s) + (term == 0 ? s_plane : 0);
-        for (uint32_t k = 0; k < side; k += 16) {
-          const uint32_t at = (k / 64) * side * 128 + (k % 64) * 2;
-          ptx::mma<1>(tmem, small_descriptor(a + at, 16), small_descriptor(b + at, 16), idesc | side / 8 << 17, term > 0 || k > 0);
-        }
+        uint32_t a = low_s + (term == 1 ? plane_s : 0), b = low_s + (term == 0 ? plane_s : 0);
+        for (uint32_t k = 0; k < side / 64; ++k, a += block, b += block)
+#pragma unroll
+          for (int u = 0; u < 4; ++u) ptx::mma<1>(tmem, ptx::descriptor(a + 2 * u), ptx::descriptor(b + 2 * u), i, term + u > 0 || k > 0);
       }
       ptx::commit<1>(ptx::smem(&bar));
     }
@@ -264,12 +267,13 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
     written();
     if (warp == 0 && ptx::elect()) {  // P X
       for (uint32_t n = 0; n < length; n += 256) {
-        const uint32_t wide = min(256u, length - n);
+        const uint32_t i = idesc | 1u << 16 | min(256u, length - n) / 8 << 17;
+#pragma unroll
         for (int term = 0; term < 3; ++term) {
-          const uint32_t a = ptx::smem(s) + (term == 1 ? s_plane : 0), b = ptx::smem(x) + (term == 0 ? x_plane : 0) + n / 64 * side * 128;
-          for (uint32_t k = 0; k < side; k += 16)
-            ptx::mma<1>(tmem + n, small_descriptor(a + (k / 64) * side * 128 + (k % 64) * 2, 16), small_descriptor(b + k * 128, side * 128),
-                        idesc | 1u << 16 | wide / 8 << 17, term > 0 || k > 0);
+          uint32_t a = low_s + (term == 1 ? plane_s : 0), b = low_xn + (term == 0 ? plane_x : 0) + n / 64 * block;
+          for (uint32_t k = 0; k < side / 64; ++k, a += block, b += 64 * 8)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) ptx::mma<1>(tmem + n, ptx::descriptor(a + 2 * u), ptx::descriptor(b + u * 128), i, term + u > 0 || k > 0);
         }
       }
       ptx::commit<1>(ptx::smem(&bar));
