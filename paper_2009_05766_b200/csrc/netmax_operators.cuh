@@ -7,7 +7,8 @@ namespace netmax {
 
 constexpr int kElementThreads = 256;
 constexpr int kPiece = 8192;        // elements of a replica that one CTA of the step's kernels works on
-constexpr int kUnroll = 4;          // rows that a thread has in flight
+template <typename T>
+constexpr int kUnroll = sizeof(T) == 4 ? 2 : 4;  // rows that a thread has in flight: 32 registers of them, and 32 of z
 
 __device__ __forceinline__ double block_sum(double v) {
   __shared__ double parts[kElementThreads / 32];
@@ -75,21 +76,77 @@ struct OperandParams {
   int32_t clear_error = 0;
 };
 
+// Eight values as they lie in memory, so that the loads of several rows are under way before the first one's arithmetic.
 template <typename T>
-__device__ __forceinline__ void operand_values(const OperandJob& j, int q, int row, int col, int count, float (&v)[8]) {
-  load8((const T*)j.src + q * j.batch + row * j.row + col, count, v);
-  if (!j.z) return;
-  float z[8];
-  load8((const T*)j.z + q * j.z_batch + row * j.z_row + col, count, z);
-  if (j.activation == kActRelu) {
+struct Eight {
+  uint32_t w[2 * sizeof(T)];
+  __device__ __forceinline__ void load(const T* at, int count, bool whole) {
+    if (whole) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] *= activation_slope(z[k], kActRelu);
-  } else if (j.activation == kActGelu) {
+      for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+        const uint4 a = ((const uint4*)at)[k];
+        w[4 * k] = a.x, w[4 * k + 1] = a.y, w[4 * k + 2] = a.z, w[4 * k + 3] = a.w;
+      }
+    } else if (sizeof(T) == 4) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] *= activation_slope(z[k], kActGelu);
-  } else {
+      for (int k = 0; k < 8; ++k)
+        if (k < (int)sizeof(T) * 2) w[k] = k < count ? ((const uint32_t*)at)[k] : 0;
+    } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] *= activation_slope(z[k], kActSilu);
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t lo = 2 * k < count ? ((const unsigned short*)at)[2 * k] : 0, hi = 2 * k + 1 < count ? ((const unsigned short*)at)[2 * k + 1] : 0;
+        w[k] = lo | hi << 16;
+      }
+    }
+  }
+  __device__ __forceinline__ float get(int k) const {
+    if (sizeof(T) == 4) return __uint_as_float(w[k]);
+    return __uint_as_float(k % 2 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
+  }
+};
+template <typename T>
+__device__ __forceinline__ bool whole_rows(const T* base, int64_t row, int count) {
+  return count == 8 && (((uintptr_t)base | (uintptr_t)(row * (int64_t)sizeof(T))) & 15) == 0;
+}
+
+// A thread's rows of matrix q, kUnroll<T> at a time: use(row, values).
+template <typename T, typename Use>
+__device__ __forceinline__ void sweep_rows(const OperandJob& j, const SweepAt& a, int q, const Use& use) {
+  if (a.count <= 0) return;
+  const T* src = (const T*)j.src + q * j.batch + a.col;
+  const T* z = j.z ? (const T*)j.z + q * j.z_batch + a.col : nullptr;
+  const bool whole = whole_rows(src, j.row, a.count), whole_z = z && whole_rows(z, j.z_row, a.count);
+  const int64_t row_stride = j.row, z_stride = j.z_row;
+  const int activation = j.activation;
+#pragma unroll 1
+  for (int row = a.row; row < a.last; row += kUnroll<T> * a.step) {
+    Eight<T> raw[kUnroll<T>], raw_z[kUnroll<T>];
+#pragma unroll
+    for (int u = 0; u < kUnroll<T>; ++u) {  // (rows past the last one repeat it: their values are not used)
+      const int64_t r = min(row + u * a.step, a.last - 1);
+      raw[u].load(src + r * row_stride, a.count, whole);
+      if (z) raw_z[u].load(z + r * z_stride, a.count, whole_z);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll<T>; ++u) {
+      if (row + u * a.step >= a.last) break;
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = raw[u].get(k);
+      if (z) {
+        if (activation == kActRelu) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] *= activation_slope(raw_z[u].get(k), kActRelu);
+        } else if (activation == kActGelu) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] *= activation_slope(raw_z[u].get(k), kActGelu);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] *= activation_slope(raw_z[u].get(k), kActSilu);
+        }
+      }
+      use(row + u * a.step, v);
+    }
   }
 }
 
@@ -120,24 +177,14 @@ __global__ __launch_bounds__(kElementThreads) void operand_maxima_kernel(const _
   const SweepAt a = sweep_at(j.sweep, blockIdx.x);
   for (int q = blockIdx.y; q < j.sweep.count; q += gridDim.y) {
     float most = 0.0f, sum[8] = {};
-    if (a.count > 0) {
-      for (int row = a.row; row < a.last; row += kUnroll * a.step) {
-        float v[kUnroll][8];
+    sweep_rows<float>(j, a, q, [&](int, const float (&v)[8]) {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-          if (row + u * a.step < a.last) operand_values<float>(j, q, row + u * a.step, a.col, a.count, v[u]);
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          if (row + u * a.step >= a.last) break;
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float m = fabsf(v[u][k]);
-            if (m <= 3.402823466e38f) most = fmaxf(most, m);
-            sum[k] += v[u][k];
-          }
-        }
+      for (int k = 0; k < 8; ++k) {
+        const float m = fabsf(v[k]);
+        if (m <= 3.402823466e38f) most = fmaxf(most, m);
+        sum[k] += v[k];
       }
-    }
+    });
     if (j.sums) write_sums(j, a, q, sum);
     if (j.maxima) {
       most = block_max(most);
@@ -168,31 +215,24 @@ __global__ __launch_bounds__(kElementThreads) void operand_kernel(const __grid_c
     }
     const float scale = ldexpf(1.0f, exponent);
     float sum[8] = {};
-    if (a.count > 0) {
-      for (int row = a.row; row < a.last; row += kUnroll * a.step) {
-        float v[kUnroll][8];
+    char* dst = (char*)j.dst + (q * j.dst_batch + a.col) * 2;
+    const int64_t dst_row = j.dst_row * 2, dst_plane = j.dst_plane * 2;
+    const bool laid = j.dst != nullptr;
+    sweep_rows<T>(j, a, q, [&](int row, float (&v)[8]) {
+      char* at = dst + row * dst_row;  // (rows are padded to eight columns)
+      if (sizeof(T) == 4) {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-          if (row + u * a.step < a.last) operand_values<T>(j, q, row + u * a.step, a.col, a.count, v[u]);
+        for (int k = 0; k < 8; ++k) v[k] *= scale;
+        uint4 hi, lo;
+        split8(v, hi, lo);
+        *(uint4*)at = hi;
+        *(uint4*)(at + dst_plane) = lo;
+      } else {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          if (row + u * a.step >= a.last) break;
-          const int64_t at = q * j.dst_batch + (row + u * a.step) * j.dst_row + a.col;  // (rows are padded to eight columns)
-          if (sizeof(T) == 4) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[u][k] *= scale;
-            uint4 hi, lo;
-            split8(v[u], hi, lo);
-            *(uint4*)((__half*)j.dst + at) = hi;
-            *(uint4*)((__half*)j.dst + at + j.dst_plane) = lo;
-          } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] += v[u][k];
-            if (j.dst) store8((__nv_bfloat16*)j.dst + at, 8, v[u]);
-          }
-        }
+        for (int k = 0; k < 8; ++k) sum[k] += v[k];
+        if (laid) store_values<__nv_bfloat16, true, 8>((__nv_bfloat16*)at, 8, v);
       }
-    }
+    });
     if (sizeof(T) == 2 && j.sums) write_sums(j, a, q, sum);
   }
 }
@@ -206,6 +246,7 @@ __global__ __launch_bounds__(kElementThreads) void column_totals_kernel(const fl
   for (int64_t e = (int64_t)blockIdx.x * kElementThreads + threadIdx.x; e < total; e += (int64_t)gridDim.x * kElementThreads) {
     const int64_t q = e / cols, col = e - q * cols;
     double s = 0.0;
+#pragma unroll 8
     for (int k = 0; k < n_parts; ++k) s += (double)parts[(q * n_parts + k) * cols + col];
     out[q * batch + col] = (T)(float)s;
   }
@@ -241,22 +282,16 @@ __global__ __launch_bounds__(kElementThreads) void norm_parts_kernel(const __gri
   ptx::wait_for_predecessor();
   if (p.clear_error && blockIdx.x + blockIdx.y == 0 && threadIdx.x == 0) *p.error = 0;
   const SweepAt a = sweep_at(p.sweep, blockIdx.x);
+  OperandJob job;
   for (int q = blockIdx.y; q < p.sweep.count; q += gridDim.y) {
     double s = 0.0;
-    if (a.count > 0) {
-      for (int row = a.row; row < a.last; row += kUnroll * a.step) {
-        float v[kUnroll][8];
+    job.src = p.u;
+    job.row = p.row;
+    job.batch = p.batch;
+    sweep_rows<T>(job, a, q, [&](int, const float (&v)[8]) {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-          if (row + u * a.step < a.last) load8((const T*)p.u + q * p.batch + (row + u * a.step) * p.row + a.col, a.count, v[u]);
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          if (row + u * a.step >= a.last) break;
-#pragma unroll
-          for (int k = 0; k < 8; ++k) s += (double)v[u][k] * (double)v[u][k];
-        }
-      }
-    }
+      for (int k = 0; k < 8; ++k) s += (double)v[k] * (double)v[k];
+    });
     s = block_sum(s);
     if (threadIdx.x == 0) p.parts[(int64_t)q * gridDim.x + blockIdx.x] = s;
   }
@@ -266,28 +301,23 @@ __global__ __launch_bounds__(kElementThreads) void first_iterate_kernel(const __
   ptx::let_successor_start();
   ptx::wait_for_predecessor();
   const SweepAt a = sweep_at(p.sweep, blockIdx.x);
+  OperandJob job;
   for (int q = blockIdx.y; q < p.sweep.count; q += gridDim.y) {
     double s = 0.0;
     for (int k = threadIdx.x; k < (int)gridDim.x; k += kElementThreads) s += p.parts[(int64_t)q * gridDim.x + k];
     const Inverse inverse = inverse_norm(block_sum(s));
-    if (a.count <= 0) continue;
-    for (int row = a.row; row < a.last; row += kUnroll * a.step) {
-      float v[kUnroll][8];
+    job.src = p.u;
+    job.row = p.row;
+    job.batch = p.batch;
+    __half* dst = p.planes + q * p.dst_batch + a.col;
+    sweep_rows<T>(job, a, q, [&](int row, float (&v)[8]) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
-        if (row + u * a.step < a.last) load8((const T*)p.u + q * p.batch + (row + u * a.step) * p.row + a.col, a.count, v[u]);
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        if (row + u * a.step >= a.last) break;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[u][k] = v[u][k] * inverse.a * inverse.b;
-        uint4 hi, lo;
-        split8(v[u], hi, lo);
-        __half* at = p.planes + q * p.dst_batch + (row + u * a.step) * p.dst_row + a.col;
-        *(uint4*)at = hi;
-        *(uint4*)(at + p.dst_plane) = lo;
-      }
-    }
+      for (int k = 0; k < 8; ++k) v[k] = v[k] * inverse.a * inverse.b;
+      uint4 hi, lo;
+      split8(v, hi, lo);
+      *(uint4*)(dst + row * p.dst_row) = hi;
+      *(uint4*)(dst + row * p.dst_row + p.dst_plane) = lo;
+    });
   }
 }
 
