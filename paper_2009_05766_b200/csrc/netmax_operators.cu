@@ -1088,6 +1088,11 @@ int enqueue_step(const netmax_step& t, int draw_stride, unsigned int* error, int
   sp.pull.workers = t.M;
   sp.error = s.error;
   const dim3 grid(plan.pieces, (unsigned)t.M);
+  if (plan.pieces > 0) {
+    sp.clear_error = s.clear;
+    s.clear = false;
+    OP_DO(launch(s, f32 ? step_momentum_kernel<float> : step_momentum_kernel<__nv_bfloat16>, grid, kElementThreads, 0, 1, sp));
+  }
   if (!plan.small.empty()) {
     SmallParams mp;
     mp.gradient = sp.gradient;
@@ -1100,6 +1105,7 @@ int enqueue_step(const netmax_step& t, int draw_stride, unsigned int* error, int
     mp.nesterov = sp.nesterov;
     mp.pull = sp.pull;
     mp.steps = t.steps;
+    mp.behind_rest = plan.pieces > 0;
     size_t smem = 0;
     uint32_t columns = 0;
     for (size_t k = 0; k < plan.small.size(); ++k) {
@@ -1111,9 +1117,6 @@ int enqueue_step(const netmax_step& t, int draw_stride, unsigned int* error, int
     OP_DO(run_small(s, mp, (unsigned)plan.small.size() * (unsigned)t.M, smem, columns,
                     f32 ? small_schulz_kernel<float, true> : small_schulz_kernel<__nv_bfloat16, true>));
   }
-  sp.clear_error = s.clear;
-  s.clear = false;
-  if (plan.pieces > 0) OP_DO(launch(s, f32 ? step_momentum_kernel<float> : step_momentum_kernel<__nv_bfloat16>, grid, kElementThreads, 0, 1, sp));
   if (!plan.groups.empty()) {
     StepIterateParams tables;
     std::memset(&tables, 0, sizeof tables);

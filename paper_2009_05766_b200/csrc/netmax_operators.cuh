@@ -391,8 +391,8 @@ constexpr int kGroupsPerThread = kPiece / (4 * kElementThreads);
 // m' = mu m + g, u = g + mu m' or m'; sums of squares of u inside matrices, the whole update outside them.
 template <typename T>
 __global__ __launch_bounds__(kElementThreads) void step_momentum_kernel(const __grid_constant__ StepParams p) {
-  ptx::let_successor_start();
   ptx::wait_for_predecessor();
+  ptx::let_successor_start();  // (in this order: see SmallParams::behind_rest)
   if (p.clear_error && blockIdx.x + blockIdx.y == 0 && threadIdx.x == 0) *p.error = 0;
   const StepSegment seg = p.segment[find_segment(p, blockIdx.x)];
   const Piece piece = piece_of(seg, blockIdx.x);

@@ -39,6 +39,9 @@ struct SmallParams {
   float ca = 0, cb = 0, cc = 0;
   unsigned int* error = nullptr;
   int32_t clear_error = 0;
+  // The launch before is the step's for everything outside small matrices.  It lets this one start when it has itself waited for what came
+  // before both, and they touch different elements: so this kernel waits for it only at its end, for the sake of the launch behind.
+  int32_t behind_rest = 0;
 };
 
 // Shared memory of a matrix: two planes of the iterate, two of S, and a block behind them (a product's 128 rows of A run past 64-row
@@ -99,7 +102,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
   if (warp == 0) ptx::tmem_alloc<1>(ptx::smem(&tmem_at), p.tmem_columns);
   for (uint32_t at = threadIdx.x * 16; at < 2 * x_plane; at += kSmallThreads * 16) *(uint4*)(x + at) = make_uint4(0, 0, 0, 0);
   ptx::let_successor_start();
-  ptx::wait_for_predecessor();
+  if (!p.behind_rest) ptx::wait_for_predecessor();
   if (p.clear_error && blockIdx.x == 0 && threadIdx.x == 0) *p.error = 0;
 
   // ---- the matrix, its norm, and the first iterate
@@ -361,6 +364,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
   __syncthreads();
   ptx::fence_after();
   if (warp == 0) ptx::tmem_free<1>(tmem, p.tmem_columns);
+  if (p.behind_rest) ptx::wait_for_predecessor();
 }
 
 }  // namespace netmax
