@@ -500,8 +500,9 @@ int netmax_layer_backward(const netmax_layer* layer);
  * Orthogonalises every matrix u: X = u / |u| (Frobenius), then `steps` times X <- a X + b (X X^T) X + c (X X^T)^2 X with
  * (a, b, c) = (3.4445, -4.7750, 2.0315): the singular values go to about 1 (between 0.68 and 1.21 after five steps for
  * values from 0.002 |u| on), the singular vectors stay.  A matrix of zeros gives zeros; one with an infinity or NaN gives NaN everywhere.
- * Iterates carry 22 bits, and so do the factors of their products; but with bfloat16 storage the factors of larger matrices (beyond a
- * smaller side of 64 and a larger one of 512, and beyond 128 and 256) are rounded to fp16 (11 bits).
+ * Iterates carry 22 bits, and so do the factors of their products; but with bfloat16 storage the factors of larger matrices are rounded
+ * to fp16 (11 bits): of those whose smaller side is above 128 or whose larger one is above 8192 (smaller side up to 64) or 4096 (up to
+ * 128), and in a step whose replicas have such a matrix also of those with a smaller side above 64 and a larger one above 256.
  */
 typedef struct netmax_orthogonal {
   int32_t count;

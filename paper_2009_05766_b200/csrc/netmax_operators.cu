@@ -857,8 +857,8 @@ OrthogonalRoom orthogonal_room(void* workspace, int count, int64_t rows, int64_t
   r.total = c.used;
   return r;
 }
-// Matrices that one CTA each orthogonalises.
-int run_small(Stream& s, SmallParams& p, unsigned blocks, size_t smem, uint32_t tmem_columns, void (*kernel)(const SmallParams)) {
+// Matrices that a CTA or a cluster each orthogonalises.
+int run_small(Stream& s, SmallParams& p, unsigned clusters, size_t smem, uint32_t tmem_columns, void (*kernel)(const SmallParams)) {
   p.tmem_columns = tmem_columns;
   p.ca = kA;
   p.cb = kB;
@@ -866,8 +866,11 @@ int run_small(Stream& s, SmallParams& p, unsigned blocks, size_t smem, uint32_t 
   p.error = s.error;
   p.clear_error = s.clear;
   s.clear = false;
+  // The CTAs of a cluster wait for one another, and a CTA for its TMEM: with one CTA per SM no two clusters hold what the other one needs.
+  if (p.ctas > 1) smem = std::max(smem, kLeastSmem);
   OP_CUDA(raise_smem_limit((const void*)kernel, smem));
-  return launch(s, kernel, dim3(blocks), kSmallThreads, smem, 1, p);
+  if (p.ctas > 8) OP_CUDA(cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  return launch(s, kernel, dim3(clusters * (unsigned)p.ctas), kSmallThreads, smem, p.ctas, p);
 }
 int check_steps(int steps) {
   if (steps < 1 || steps > 20) return fail_op(NETMAX_INVALID_ARG, "steps = %d outside [1, 20]", steps);
@@ -911,7 +914,9 @@ int netmax_orthogonalise(const netmax_orthogonal* o) try {
     sp.rows = (int32_t)o->rows;
     sp.cols = (int32_t)o->cols;
     sp.steps = o->steps;
-    return run_small(s, sp, (unsigned)o->count, small_smem((uint32_t)o->rows, (uint32_t)o->cols), small_tmem((uint32_t)o->rows, (uint32_t)o->cols),
+    const uint32_t rows = (uint32_t)o->rows, cols = (uint32_t)o->cols;
+    sp.ctas = (int32_t)small_ctas(o->count, rows, cols, sm_count());
+    return run_small(s, sp, (unsigned)o->count, small_smem(rows, cols, sp.ctas), small_tmem(rows, cols, sp.ctas),
                      f32 ? small_schulz_kernel<float, false> : small_schulz_kernel<__nv_bfloat16, false>);
   }
   SchulzGroup& q = room.group;
@@ -959,7 +964,7 @@ int netmax_workspace_status(const void* workspace, int32_t device, void* stream)
 namespace {
 
 struct StepPlan {
-  std::vector<netmax_matrix> small;    // those that one CTA orthogonalises
+  std::vector<netmax_matrix> small;    // those that a CTA or a cluster orthogonalises
   std::vector<netmax_matrix> sorted;   // the others by shape, then by offset: the order of the tables
   std::vector<SchulzGroup> groups;     // of equal shapes
   std::vector<int> first;              // of a group, in `sorted`
@@ -983,7 +988,10 @@ int plan_step(int32_t M, int64_t d, const netmax_matrix* matrices, int32_t n, in
     if (!std::isfinite(m.scale)) return fail_op(NETMAX_INVALID_ARG, "the scale of the matrix at %lld is not finite", (long long)m.offset);
     if ((int64_t)M * m.rows * m.cols >= (int64_t)1 << 40) return fail_op(NETMAX_INVALID_ARG, "M matrices of %lld x %lld are too many", (long long)m.rows, (long long)m.cols);
   }
-  const auto apart = std::stable_partition(plan.sorted.begin(), plan.sorted.end(), [](const netmax_matrix& m) { return !is_small(m.rows, m.cols); });
+  const bool larger = std::any_of(plan.sorted.begin(), plan.sorted.end(), [](const netmax_matrix& m) { return !is_small(m.rows, m.cols); });
+  const auto apart = std::stable_partition(plan.sorted.begin(), plan.sorted.end(), [&](const netmax_matrix& m) {
+    return !is_small(m.rows, m.cols) || (larger && joins_larger(m.rows, m.cols));
+  });
   plan.small.assign(apart, plan.sorted.end());
   plan.sorted.erase(apart, plan.sorted.end());
   std::sort(plan.sorted.begin(), plan.sorted.end(), [](const netmax_matrix& a, const netmax_matrix& b) {
@@ -1093,8 +1101,24 @@ int enqueue_step(const netmax_step& t, int draw_stride, unsigned int* error, int
     s.clear = false;
     OP_DO(launch(s, f32 ? step_momentum_kernel<float> : step_momentum_kernel<__nv_bfloat16>, grid, kElementThreads, 0, 1, sp));
   }
-  if (!plan.small.empty()) {
+  // The small matrices, those that need equally large clusters in one launch; only the first of these runs beside the rest.
+  std::vector<uint32_t> needs(plan.small.size());
+  for (size_t k = 0; k < plan.small.size(); ++k)
+    needs[k] = small_ctas((int64_t)plan.small.size() * t.M, (uint32_t)plan.small[k].rows, (uint32_t)plan.small[k].cols, sm_count());
+  bool beside = plan.pieces > 0;
+  for (uint32_t ctas = 1; ctas <= kMostCtas; ctas *= 2) {
     SmallParams mp;
+    unsigned n = 0;
+    size_t smem = 0;
+    uint32_t columns = 0;
+    for (size_t k = 0; k < plan.small.size(); ++k) {
+      if (needs[k] != ctas) continue;
+      const netmax_matrix& m = plan.small[k];
+      mp.matrix[n++] = {(uint32_t)m.offset, (uint32_t)m.rows, (uint32_t)m.cols, (float)m.scale};
+      smem = std::max(smem, small_smem((uint32_t)m.rows, (uint32_t)m.cols, ctas));
+      columns = std::max(columns, small_tmem((uint32_t)m.rows, (uint32_t)m.cols, ctas));
+    }
+    if (n == 0) continue;
     mp.gradient = sp.gradient;
     mp.gradient_row = sp.gradient_row;
     mp.momentum = sp.momentum;
@@ -1105,17 +1129,10 @@ int enqueue_step(const netmax_step& t, int draw_stride, unsigned int* error, int
     mp.nesterov = sp.nesterov;
     mp.pull = sp.pull;
     mp.steps = t.steps;
-    mp.behind_rest = plan.pieces > 0;
-    size_t smem = 0;
-    uint32_t columns = 0;
-    for (size_t k = 0; k < plan.small.size(); ++k) {
-      const netmax_matrix& m = plan.small[k];
-      mp.matrix[k] = {(uint32_t)m.offset, (uint32_t)m.rows, (uint32_t)m.cols, (float)m.scale};
-      smem = std::max(smem, small_smem((uint32_t)m.rows, (uint32_t)m.cols));
-      columns = std::max(columns, small_tmem((uint32_t)m.rows, (uint32_t)m.cols));
-    }
-    OP_DO(run_small(s, mp, (unsigned)plan.small.size() * (unsigned)t.M, smem, columns,
-                    f32 ? small_schulz_kernel<float, true> : small_schulz_kernel<__nv_bfloat16, true>));
+    mp.ctas = (int32_t)ctas;
+    mp.behind_rest = beside;
+    beside = false;
+    OP_DO(run_small(s, mp, n * (unsigned)t.M, smem, columns, f32 ? small_schulz_kernel<float, true> : small_schulz_kernel<__nv_bfloat16, true>));
   }
   if (!plan.groups.empty()) {
     StepIterateParams tables;

@@ -1,12 +1,16 @@
-// Newton-Schulz orthogonalisation of small matrices (smaller side up to 64 with a larger one up to 512, or up to 128 and 256): a CTA per
-// matrix, everything in one launch.
+// Newton-Schulz orthogonalisation of small and of long, thin matrices (smaller side up to 64 with a larger one up to 8192; up to 128 and
+// 4096): a CTA or a cluster of CTAs per matrix, everything in one launch.
 //
-// The general path is 15 products and two sweeps, each a launch of 5-7 us whose work is far below a microsecond for such sizes (four
-// 64 x 64 matrices: 112 us).  Here the iterate stays in shared memory as two fp16 planes in the tensor cores' own layout (blocks of 64
-// columns, rows of 128 bytes, 16-byte pieces swizzled by the row), S = X X^T and the polynomial beside it, accumulators in TMEM; a
-// step is three rounds of products, wait, 16 columns a thread, barrier.  The one layout serves as k-contiguous operand (X X^T, S S, P) and as
-// n-contiguous one (X in P X).  Tall matrices are transposed on their way in and out.  All products take the three terms of two-plane factors,
-// whatever the storage: they cost nothing here.  Sums over more than 128 columns of X go to accumulators of their own, added in fp32.
+// The general path is 15 products and two sweeps, each a launch of 5-7 us whose work is far below a microsecond for small sizes (four
+// 64 x 64 matrices: 112 us); of long, thin ones its sums over the length run on one CTA (three of 27 x 4024: 205 us).  Here the iterate
+// stays in shared memory as two fp16 planes in the tensor cores' own layout (blocks of 64 columns, rows of 128 bytes, 16-byte pieces
+// swizzled by the row), S = X X^T and the polynomial beside it, accumulators in TMEM; a step is three rounds of products, wait, 16 columns
+// a thread, barrier.  The one layout serves as k-contiguous operand (X X^T, S S, P) and as n-contiguous one (X in P X).  Tall matrices are
+// transposed on their way in and out.  All products take the three terms of two-plane factors, whatever the storage: they cost little here.
+// Sums over more than 128 columns of X go to accumulators of their own, added in fp32.
+//
+// The CTAs of a cluster share out the columns of X.  Each adds up one part of the rows of S over all of them, in their order, through
+// distributed shared memory, and gives every CTA its planes; what follows from S they all work out for themselves.
 #pragma once
 #include "netmax_operators.cuh"
 
@@ -24,7 +28,7 @@ struct SmallParams {
   int64_t row = 0, batch = 0;
   void* out = nullptr;
   int64_t out_row = 0, out_batch = 0;
-  // or inside replicas: matrix blockIdx.x / workers of worker blockIdx.x % workers
+  // or inside replicas: matrix q / workers of worker q % workers, for the q-th cluster
   const void* gradient = nullptr;
   int64_t gradient_row = 0;
   const float* momentum = nullptr;
@@ -35,6 +39,7 @@ struct SmallParams {
   PullParams pull;
   SmallMatrix matrix[kMaxMatrices];
   int32_t rows = 0, cols = 0, steps = 0;
+  int32_t ctas = 1;  // of a cluster
   uint32_t tmem_columns = 0;
   float ca = 0, cb = 0, cc = 0;
   unsigned int* error = nullptr;
@@ -47,22 +52,54 @@ struct SmallParams {
 // Shared memory of a matrix: two planes of the iterate, two of S, and a block behind them (a product's 128 rows of A run past 64-row
 // blocks; what they find there reaches only rows of the accumulator that nobody reads).
 __host__ __device__ inline uint32_t small_side(uint32_t rows, uint32_t cols) { return (rows < cols ? rows : cols) <= 64 ? 64 : 128; }
-__host__ __device__ inline uint32_t small_length(uint32_t rows, uint32_t cols) { return ((rows < cols ? cols : rows) + 63) / 64 * 64; }
-__host__ __device__ inline bool is_small(int64_t rows, int64_t cols) {
-  const int64_t side = rows < cols ? rows : cols, length = rows < cols ? cols : rows;
-  return (side <= 64 && length <= 512) || (side <= 128 && length <= 256);
+// Columns of the iterate that a CTA of a cluster holds.
+__host__ __device__ inline uint32_t small_slice(uint32_t rows, uint32_t cols, uint32_t ctas) {
+  return (((rows < cols ? cols : rows) + ctas - 1) / ctas + 63) / 64 * 64;
 }
-inline size_t small_smem(uint32_t rows, uint32_t cols) {
-  const size_t r = small_side(rows, cols), l = small_length(rows, cols);
+constexpr uint32_t kMostCtas = 16;
+__host__ __device__ inline uint32_t most_columns(uint32_t side) { return side == 64 ? 512 : 256; }
+inline uint32_t least_ctas(uint32_t rows, uint32_t cols) {
+  uint32_t c = 1;
+  while (small_slice(rows, cols, c) > most_columns(small_side(rows, cols))) c *= 2;
+  return c;
+}
+// Whether matrices take this path (us, this / the general path, five steps of fp32: 24 of 128 x 1152 199 / 234, 32 of 128 x 4096 600 / 783).
+inline bool is_small(int64_t rows, int64_t cols) {
+  const int64_t side = rows < cols ? rows : cols, length = rows < cols ? cols : rows;
+  return side <= 128 && length <= (int64_t)kMostCtas * most_columns(side <= 64 ? 64 : 128);
+}
+// Of these, the ones that a step leaves to the general path where that has larger matrices to run anyway: adding up 128 x 128 parts costs a
+// cluster about as much as the rest of its work, and in launches that are there already they cost less (the update of 8 ResNet18-sized
+// replicas 3850 us, with these apart 3990).
+inline bool joins_larger(int64_t rows, int64_t cols) { return (rows < cols ? rows : cols) > 64 && least_ctas((uint32_t)rows, (uint32_t)cols) > 1; }
+// CTAs for each of `count` matrices: as many as hold one; with sides up to 64 more while SMs would be idle and slices are long, but of
+// clusters of sixteen no more than surely run at once (nine of 3726 x 11 in eights 78 us, in sixteens 116).
+inline uint32_t small_ctas(int64_t count, uint32_t rows, uint32_t cols, int sms) {
+  uint32_t c = least_ctas(rows, cols);
+  while (small_side(rows, cols) == 64 && c < kMostCtas && small_slice(rows, cols, c) > 128 && count * c * 2 <= (c < 8 ? sms : 64)) c *= 2;
+  return c;
+}
+inline size_t small_smem(uint32_t rows, uint32_t cols, uint32_t ctas) {
+  const size_t r = small_side(rows, cols), l = small_slice(rows, cols, ctas);
   return 1024 + 2 * r * l * 2 + 2 * r * r * 2 + kBoxBytes;
 }
-inline uint32_t small_tmem(uint32_t rows, uint32_t cols) {
-  const uint32_t r = small_side(rows, cols), l = small_length(rows, cols), need = l > (l + 127) / 128 * r ? l : (l + 127) / 128 * r;
+inline uint32_t small_tmem(uint32_t rows, uint32_t cols, uint32_t ctas) {
+  const uint32_t r = small_side(rows, cols), l = small_slice(rows, cols, ctas), need = l > (l + 127) / 128 * r ? l : (l + 127) / 128 * r;
   uint32_t c = 32;
   while (c < need) c *= 2;
   return c;
 }
 
+// Another CTA's shared memory.
+__device__ __forceinline__ float4 load_remote(uint32_t at) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void store_remote(uint32_t at, uint4 v) {
+  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void store_remote(uint32_t at, double v) { asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(at), "d"(v) : "memory"); }
 __device__ __forceinline__ void tmem_load16(uint32_t at, float (&v)[16]) {
   uint32_t r[16];
   __syncwarp();
@@ -85,13 +122,16 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
   extern __shared__ unsigned char raw[];
   __shared__ __align__(8) uint64_t bar;
   __shared__ uint32_t tmem_at;
-  __shared__ double squares[kSmallThreads / 32];
+  __shared__ double squares[kSmallThreads / 32], norms[kMostCtas];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   unsigned char* const base = raw + (((ptx::smem(raw) + 1023) & ~1023u) - ptx::smem(raw));
-  const int worker = kStep ? blockIdx.x % p.pull.workers : 0, which = kStep ? blockIdx.x / p.pull.workers : 0;
+  const uint32_t ctas = p.ctas, rank = blockIdx.x % ctas, matrix = blockIdx.x / ctas;
+  const int worker = kStep ? matrix % p.pull.workers : 0, which = kStep ? matrix / p.pull.workers : 0;
   const uint32_t rows = kStep ? p.matrix[which].rows : (uint32_t)p.rows, cols = kStep ? p.matrix[which].cols : (uint32_t)p.cols;
   const bool tall = rows > cols;
-  const uint32_t side = small_side(rows, cols), length = small_length(rows, cols);
+  const uint32_t side = small_side(rows, cols), length = small_slice(rows, cols, ctas);
+  const uint32_t begin = rank * length, whole_length = tall ? rows : cols;           // this CTA's columns of the iterate
+  const uint32_t own = begin < whole_length ? min(length, whole_length - begin) : 0;  // that exist
   const uint32_t x_plane = side * length * 2, s_plane = side * side * 2;
   unsigned char* const x = base;
   unsigned char* const s = base + 2 * x_plane;
@@ -106,7 +146,8 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
   if (p.clear_error && blockIdx.x == 0 && threadIdx.x == 0) *p.error = 0;
 
   // ---- the matrix, its norm, and the first iterate
-  const uint32_t groups_per_row = (cols + 7) / 8, groups = rows * groups_per_row;  // at most 4096 of eight columns
+  const uint32_t own_rows = tall ? own : rows, own_cols = tall ? cols : own, first_row = tall ? begin : 0, first_col = tall ? 0 : begin;
+  const uint32_t groups_per_row = max(1u, (own_cols + 7) / 8), groups = own_cols ? own_rows * groups_per_row : 0;  // at most 4096 of eight columns
   float u[8][8];
   double sum = 0.0;
 #pragma unroll
@@ -114,9 +155,9 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
     const uint32_t group = i * kSmallThreads + threadIdx.x;
     if (group >= groups) break;
     const uint32_t row = group / groups_per_row, col = (group - row * groups_per_row) * 8;
-    const int count = min(8u, cols - col);
+    const int count = min(8u, own_cols - col);
     if (kStep) {
-      const int64_t at = (int64_t)p.matrix[which].offset + row * cols + col;
+      const int64_t at = (int64_t)p.matrix[which].offset + (first_row + row) * cols + first_col + col;
       float grad[8];
       load8((const T*)p.gradient + worker * p.gradient_row + at, count, grad);
       load8(p.momentum + worker * p.momentum_row + at, count, u[i]);
@@ -127,7 +168,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
       for (int k = 0; k < 8; ++k)
         if (p.nesterov) u[i][k] = fmaf(p.mu, u[i][k], grad[k]);
     } else {
-      load8((const T*)p.u + blockIdx.x * p.batch + row * p.row + col, count, u[i]);
+      load8((const T*)p.u + matrix * p.batch + (first_row + row) * p.row + first_col + col, count, u[i]);
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum += (double)u[i][k] * (double)u[i][k];  // (columns that are not there are zeros)
@@ -142,6 +183,13 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
   sum = 0.0;
 #pragma unroll
   for (int w = 0; w < kSmallThreads / 32; ++w) sum += squares[w];
+  if (ctas > 1) {
+    ptx::cluster_sync();  // (every CTA of the cluster runs)
+    if (threadIdx.x < ctas) store_remote(ptx::map_to(ptx::smem(&norms[rank]), threadIdx.x), sum);
+    ptx::cluster_sync();
+    sum = 0.0;
+    for (uint32_t r = 0; r < ctas; ++r) sum += norms[r];
+  }
   const Inverse inverse = inverse_norm(sum);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -159,7 +207,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
       const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        if (col + k >= cols) break;
+        if (col + k >= own_cols) break;
         const uint32_t at = small_at(side, col + k, row);
         *(unsigned short*)(x + at) = (unsigned short)(h[k / 2] >> (16 * (k % 2)));
         *(unsigned short*)(x + x_plane + at) = (unsigned short)(l[k / 2] >> (16 * (k % 2)));
@@ -183,19 +231,16 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
     ++phase;
     ptx::fence_after();
   };
-  // What threads have stored is there for the tensor cores.  With 64 rows the warps of the accumulator's upper half have no more to do.
-  const int busy = side == 64 ? kSmallThreads / 2 : kSmallThreads;
-  auto written = [&] {
+  auto written = [&] {  // what threads have stored is there for the tensor cores
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     ptx::fence_before();
-    asm volatile("bar.sync 1, %0;" ::"r"(busy) : "memory");
+    __syncthreads();
     ptx::fence_after();
   };
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  ptx::fence_before();
-  __syncthreads();
-  ptx::fence_after();
-  for (int step = 0; step < p.steps && live; ++step) {
+  // S's parts before they are added up: fp32, in the place of its planes, 16-byte pieces swizzled by the row.
+  auto part_at = [&](uint32_t row, uint32_t piece) { return row * side * 4 + ((piece ^ (row & 7)) * 16); };
+  written();
+  for (int step = 0; step < p.steps; ++step) {
     const bool last = step + 1 == p.steps;
     if (warp == 0 && ptx::elect()) {  // S = X X^T
       for (uint32_t part = 0; part < parts; ++part) {
@@ -212,7 +257,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
     }
     __syncwarp();
     products_done();
-    {
+    if (live) {
       for (uint32_t c = (warp / 4) * 16; c < side; c += 64) {
         float v[16], w[16];
         tmem_load16(from + c, v);
@@ -220,6 +265,11 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
           tmem_load16(from + part * side + c, w);
 #pragma unroll
           for (int k = 0; k < 16; ++k) v[k] += w[k];
+        }
+        if (ctas > 1) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) *(float4*)(s + part_at(m, c / 4 + k)) = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+          continue;
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -233,7 +283,44 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
         }
       }
     }
-    written();
+    if (ctas > 1) {  // rows rank * side / ctas ... of S, eight columns a thread
+      const uint32_t share = side / ctas * (side / 8);
+      float t[2][8] = {};  // (two CTAs share out 128 x 128: two pieces a thread, otherwise at most one)
+      ptx::fence_before();
+      ptx::cluster_sync();  // all parts are there
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t piece = i * kSmallThreads + threadIdx.x;
+        if (piece >= share) break;
+        const uint32_t row = rank * (side / ctas) + piece / (side / 8), col = piece % (side / 8) * 8;
+        for (uint32_t r = 0; r < ctas; ++r) {
+          const float4 a = load_remote(ptx::map_to(ptx::smem(s) + part_at(row, col / 4), r)), b = load_remote(ptx::map_to(ptx::smem(s) + part_at(row, col / 4 + 1), r));
+          t[i][0] += a.x, t[i][1] += a.y, t[i][2] += a.z, t[i][3] += a.w, t[i][4] += b.x, t[i][5] += b.y, t[i][6] += b.z, t[i][7] += b.w;
+        }
+      }
+      ptx::cluster_sync();  // all have been read
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t piece = i * kSmallThreads + threadIdx.x;
+        if (piece >= share) break;
+        const uint32_t row = rank * (side / ctas) + piece / (side / 8), col = piece % (side / 8) * 8;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[i][k] *= kPlaneUnscale;
+        uint4 hi, lo;
+        split8(t[i], hi, lo);
+        for (uint32_t r = 0; r < ctas; ++r) {
+          const uint32_t at = ptx::map_to(ptx::smem(s) + small_at(side, row, col), r);
+          store_remote(at, hi);
+          store_remote(at + s_plane, lo);
+        }
+      }
+      asm volatile("fence.proxy.async;" ::: "memory");
+      ptx::cluster_sync();  // every CTA has all of S
+      asm volatile("fence.proxy.async;" ::: "memory");
+      ptx::fence_after();
+    } else {
+      written();
+    }
     if (warp == 0 && ptx::elect()) {  // S S
       const uint32_t i = idesc | side / 8 << 17;
 #pragma unroll
@@ -247,7 +334,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
     }
     __syncwarp();
     products_done();
-    {
+    if (live) {
       for (uint32_t c = (warp / 4) * 16; c < side; c += 64) {  // P = b S + c S S in S's place: every thread reads what it writes
         float v[16];
         tmem_load16(from + c, v);
@@ -283,7 +370,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
     }
     __syncwarp();
     products_done();
-    {
+    if (live) {
       for (uint32_t c = (warp / 4) * 16; c < length; c += 64) {
         float v[16];
         tmem_load16(from + c, v);
@@ -304,13 +391,13 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
             continue;
           }
           // row m, columns c + 8 h ... of the iterate: a row of the matrix, or a piece of eight of its rows' column m
-          const uint32_t col = c + 8 * h;
-          if (m >= (tall ? cols : rows) || col >= (tall ? rows : cols)) continue;
-          const int count = min(8u, (tall ? rows : cols) - col);
+          if (m >= (tall ? cols : rows) || c + 8 * h >= own) continue;
+          const int count = min(8u, own - (c + 8 * h));
+          const uint32_t col = begin + c + 8 * h;
 #pragma unroll
           for (int k = 0; k < 8; ++k) t[k] *= kPlaneUnscale;
           if (!kStep) {
-            T* out = (T*)p.out + blockIdx.x * p.out_batch;
+            T* out = (T*)p.out + matrix * p.out_batch;
             if (!tall) {
               store8(out + m * p.out_row + col, count, t);
             } else {
@@ -362,6 +449,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
   }
   ptx::fence_before();
   __syncthreads();
+  if (ctas > 1) ptx::cluster_sync();  // (no CTA's shared memory goes while another one may still use it)
   ptx::fence_after();
   if (warp == 0) ptx::tmem_free<1>(tmem, p.tmem_columns);
   if (p.behind_rest) ptx::wait_for_predecessor();

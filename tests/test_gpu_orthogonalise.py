@@ -9,7 +9,7 @@ The errors are spread like noise over the directions, so their factors are taken
 fp32: u = 2^-20 (22-bit factors; 48 steps between two fp32 sums, each of which drops less than 2^-24 of a running sum that is half the
 final one on average and whose terms have both signs: at most 24 2^-24 = 1.5 2^-20 if they had one, and C, which takes every part at its
 largest, has that much room).
-Small matrices (side up to 64 and length up to 512, or 128 and 256) have 22-bit factors with bfloat16 storage as well: u = 2^-20, and the
+Small matrices (see is_small) have 22-bit factors with bfloat16 storage as well: u = 2^-20, and the
 result's rounding, 2^-8 of itself.
 bfloat16, larger: the factors' rounding to fp16 is part of the definition (u = 2^-12); the emulation rounds at the same places in 64 bits, and the
 kernel may differ from it by the rounding of the result (2^-8 of itself, and in the root mean square less than 0.6 of that, which leaves
@@ -99,7 +99,13 @@ def orthogonalise(nm, u, steps=5):
 
 def is_small(rows, cols):
     side, length = min(rows, cols), max(rows, cols)
-    return (side <= 64 and length <= 512) or (side <= 128 and length <= 256)
+    return (side <= 64 and length <= 8192) or (side <= 128 and length <= 4096)
+
+
+def is_narrow(rows, cols, matrices):
+    """Whether a step rounds this one's factors to fp16 with bfloat16 storage."""
+    larger = any(not is_small(r, c) for _, r, c, _ in matrices)
+    return not is_small(rows, cols) or (larger and min(rows, cols) > 64 and max(rows, cols) > 256)
 
 
 def check(got, u, steps=5):
@@ -114,7 +120,10 @@ def check(got, u, steps=5):
 
 
 SIZES = [(1, 1, 1), (2, 1, 9), (2, 9, 1), (3, 5, 7), (4, 64, 64), (2, 64, 27), (1, 27, 64), (2, 130, 131), (3, 65, 300), (2, 300, 65), (1, 128, 128),
-         (1, 129, 512), (2, 256, 256), (5, 257, 255), (2, 600, 520), (33, 40, 24), (1, 1003, 777), (2, 512, 1536), (3, 1100, 1100)]
+         (1, 129, 512), (2, 256, 256), (5, 257, 255), (2, 600, 520), (33, 40, 24), (1, 1003, 777), (2, 512, 1536), (3, 1100, 1100),
+         (3, 27, 4024), (2, 3726, 11), (3, 97, 2513), (1, 128, 4096), (1, 8192, 64), (2, 64, 8191), (1, 8193, 64), (1, 128, 4097), (4, 64, 512), (40, 100, 256),
+         (5, 65, 1025), (1, 1, 5000), (20, 31, 956), (7, 600, 128),
+         (75, 70, 300), (74, 300, 70)]
 
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
@@ -212,7 +221,7 @@ def exact_step(x, m, grad, matrices, peers, weights, lr, mu, nesterov, decay, st
     o, off = u.clone(), 2.0 ** -22 * u.abs()
     for at, rows, cols, scale in matrices:
         part = u[:, at:at + rows * cols].reshape(-1, rows, cols)
-        narrow = f16 and not is_small(rows, cols)
+        narrow = f16 and is_narrow(rows, cols, matrices)
         found = iterates(part, steps, fp16=narrow)
         o[:, at:at + rows * cols] = scale * found[-1].reshape(-1, rows * cols)
         # (the emulation's and the kernel's iterates differ by rounded factors: see above; 2-norms bound every element)
@@ -228,6 +237,7 @@ def exact_step(x, m, grad, matrices, peers, weights, lr, mu, nesterov, decay, st
 
 
 CASES = [  # M, d, matrices
+    (3, 130003, [(0, 70, 500, 1.0), (35003, 200, 300, 1.0), (95003, 60, 500, 2.0), (125003, 8, 600, 1.0)]), (3, 70002, [(1, 70, 500, 1.0), (35002, 500, 70, 1.0)]),
     (2, 1, []), (3, 5000, []), (4, 4096, [(0, 64, 48, 1.0)]), (3, 4097, [(1, 64, 64, 2.0)]), (5, 9001, [(3, 31, 77, 1.0), (2391, 77, 31, 0.5), (5000, 31, 77, 1.5), (7387, 1, 1614, 1.0)]),
     (2, 200000, [(0, 300, 300, 1.0), (90000, 300, 300, 1.0), (180001, 10, 512, 3.0)]),
 ]

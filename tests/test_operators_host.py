@@ -110,7 +110,7 @@ BAD_TABLES = [tables((990, 4, 4, 1.0)), tables((-1, 4, 4, 1.0)), tables((0, 0, 4
     (dict(momentum=NONE), -1), (dict(momentum_next=NONE), -1), (dict(peers=None), -1), (dict(weights=None), -1), (dict(lr=float("nan")), -1),
     (dict(mu=float("inf")), -1), (dict(decay=float("nan")), -1), (dict(steps=0), -1), (dict(x_next=view(0, 1000, 1000)), -1), (dict(x_next=view(2, 1000, 1000)), -1),
     (dict(x_next=view(1, 1000, 999)), -1), (dict(momentum_next=view(1, 1000, 1000)), -1), (dict(momentum_next=b.View(BASE + (3 << 36) + 4, 1000, 1000)), -1),
-    (dict(n_matrices=-1), -1), (dict(n_matrices=257), -1), (dict(matrices=None), -1), (dict(workspace=None), -1), (dict(workspace_bytes=512), -3)]
+    (dict(n_matrices=-1), -1), (dict(n_matrices=257), -1), (dict(matrices=None), -1), (dict(workspace=None), -1), (dict(workspace_bytes=256), -3)]
     + [(dict(matrices=C.addressof(t), n_matrices=len(t)), -1) for t in BAD_TABLES])
 def test_step_refuses(changes, code):
     assert code_of(b.lib().netmax_orthogonalised_step, step(**changes)) == code
@@ -133,8 +133,8 @@ def test_workspace_sizes_hold_what_the_kernels_use():
     assert b.netmax_layer_workspace_size(2, 10, 9, 7, "f32") >= 2 * 4 * (10 * 16 + 7 * 16 + 10 * 8)
     assert b.netmax_layer_workspace_size(2, 10, 9, 7, "bf16") >= 2 * 2 * (10 * 16 + 7 * 16 + 10 * 8)
     assert b.netmax_orthogonalise_workspace_size(5, 11, 13, "f32") >= 5 * (2 * 4 * 11 * 16 + 2 * 4 * 11 * 16)
-    table = [(0, 11, 13, 1.0), (143, 13, 11, 1.0)]
-    assert b.netmax_orthogonalised_step_workspace_size(5, 286, table, "f32") >= 5 * (2 * 4 * 11 * 16 + 2 * 4 * 11 * 16)
+    table = [(0, 211, 213, 1.0), (44943, 213, 211, 1.0)]    # (matrices that one CTA holds need none)
+    assert b.netmax_orthogonalised_step_workspace_size(5, 89886, table, "f32") >= 2 * 5 * (2 * 4 * 211 * 216 + 2 * 4 * 211 * 216)
 
 
 @pytest.mark.parametrize("struct,name", [(b.View, "netmax_view"), (b.Layer, "netmax_layer"), (b.Orthogonal, "netmax_orthogonal"), (b.Matrix, "netmax_matrix"),
