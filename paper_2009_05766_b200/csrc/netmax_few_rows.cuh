@@ -78,4 +78,148 @@ __global__ __launch_bounds__(kElementThreads) void few_rows_kernel(const __grid_
   ((T*)p.y)[q * p.y_batch + r * p.y_row + o] = (T)mine;
 }
 
+// ---- the gradient of such batches: bound by writing dW and reading W once ----------------------
+// A thread has kN neighbouring columns of n_in, `1 << shift` threads a row; dz of 64 outputs at a time goes through shared memory.
+constexpr int kFewOutputs = 64;
+struct FewRowsBackParams {
+  const void *dy = nullptr, *z = nullptr, *x = nullptr, *weight = nullptr;
+  void *dx = nullptr, *dweight = nullptr, *dbias = nullptr;
+  int64_t dy_row = 0, dy_batch = 0, z_row = 0, z_batch = 0, x_row = 0, x_batch = 0, weight_row = 0, weight_batch = 0, dx_row = 0, dx_batch = 0, dweight_row = 0,
+          dweight_batch = 0, dbias_batch = 0;
+  int32_t M = 0, n = 0, n_in = 0, n_out = 0, activation = 0;
+  int32_t shift = 0, col_tiles = 1, outputs_per_block = kFewOutputs, chunks = 1;
+  float* parts = nullptr;  // [chunks][M][n][n_in] of dx
+  unsigned int* error = nullptr;
+  int32_t clear_error = 0;
+};
+
+template <typename T>
+__device__ __forceinline__ void stage_dz(const FewRowsBackParams& p, int64_t q, int first, float (*dz)[kFewOutputs]) {
+  for (int e = threadIdx.x; e < p.n * kFewOutputs; e += kElementThreads) {
+    const int r = e / kFewOutputs, o = first + e % kFewOutputs;
+    float v = 0.0f;
+    if (o < p.n_out) {
+      v = (float)((const T*)p.dy)[q * p.dy_batch + r * p.dy_row + o];
+      if (p.z) v *= activation_slope((float)((const T*)p.z)[q * p.z_batch + r * p.z_row + o], p.activation);
+    }
+    dz[r][e % kFewOutputs] = v;
+  }
+}
+
+// dW and the sums of dz.
+template <typename T, int kRows>
+__global__ __launch_bounds__(kElementThreads) void few_rows_dweight_kernel(const __grid_constant__ FewRowsBackParams p) {
+  constexpr int kN = 16 / sizeof(T);
+  __shared__ float dz[kRows][kFewOutputs];
+  ptx::let_successor_start();
+  ptx::wait_for_predecessor();
+  if (p.clear_error && blockIdx.x + blockIdx.y == 0 && threadIdx.x == 0) *p.error = 0;
+  const int64_t q = blockIdx.y;
+  const int tile = blockIdx.x % p.col_tiles, first = blockIdx.x / p.col_tiles * kFewOutputs;
+  const int col = ((tile << p.shift) + (threadIdx.x & ((1 << p.shift) - 1))) * kN, count = min(kN, p.n_in - col);
+  stage_dz<T>(p, q, first, dz);
+  __syncthreads();
+  if (p.dbias && tile == 0)
+    for (int o = threadIdx.x; o < kFewOutputs && first + o < p.n_out; o += kElementThreads) {
+      float s = 0.0f;
+      for (int r = 0; r < p.n; ++r) s += dz[r][o];
+      ((T*)p.dbias)[q * p.dbias_batch + first + o] = (T)s;
+    }
+  if (!p.dweight || count <= 0) return;
+  float x[kRows][kN];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+#pragma unroll
+    for (int k = 0; k < kN; ++k) x[r][k] = 0.0f;
+    if (r < p.n) load_values<T, false, kN>((const T*)p.x + q * p.x_batch + r * p.x_row + col, count, x[r]);
+  }
+  const int step = kElementThreads >> p.shift, n = p.n;
+  T* out = (T*)p.dweight + q * p.dweight_batch + first * p.dweight_row + col;
+  const int64_t row = p.dweight_row;
+  for (int o = threadIdx.x >> p.shift; o < kFewOutputs && first + o < p.n_out; o += step) {
+    float v[kN] = {};
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      if (r >= n) break;
+      const float d = dz[r][o];
+#pragma unroll
+      for (int k = 0; k < kN; ++k) v[k] = fmaf(d, x[r][k], v[k]);
+    }
+    store_values<T, false, kN>(out + o * row, count, v);
+  }
+}
+
+// dx, or its part of a block's outputs.
+template <typename T, int kRows>
+__global__ __launch_bounds__(kElementThreads) void few_rows_dx_kernel(const __grid_constant__ FewRowsBackParams p) {
+  constexpr int kN = 16 / sizeof(T);
+  __shared__ float dz[kRows][kFewOutputs];
+  __shared__ float sums[kElementThreads][kN];
+  ptx::let_successor_start();
+  ptx::wait_for_predecessor();
+  if (p.clear_error && blockIdx.x + blockIdx.y == 0 && threadIdx.x == 0) *p.error = 0;
+  const int64_t q = blockIdx.y;
+  const int tile = blockIdx.x % p.col_tiles, chunk = blockIdx.x / p.col_tiles, begin = chunk * p.outputs_per_block, end = min(p.n_out, begin + p.outputs_per_block);
+  const int lanes = 1 << p.shift, lane = threadIdx.x & (lanes - 1), at = threadIdx.x >> p.shift, step = kElementThreads >> p.shift;
+  const int col = ((tile << p.shift) + lane) * kN, count = min(kN, p.n_in - col), n = p.n;
+  float acc[kRows][kN] = {};
+  const T* w = (const T*)p.weight + q * p.weight_batch + col;
+  const int64_t row = p.weight_row;
+  for (int first = begin; first < end; first += kFewOutputs) {
+    __syncthreads();
+    stage_dz<T>(p, q, first, dz);
+    __syncthreads();
+    if (count <= 0) continue;
+    const int last = min(kFewOutputs, end - first);
+    for (int o = at; o < last; o += 4 * step) {
+      float a[4][kN];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)  // (outputs past the last one repeat it, with a zero for dz)
+        load_values<T, false, kN>(w + (int64_t)(first + min(o + u * step, last - 1)) * row, count, a[u]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const bool live = o + u * step < last;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          if (r >= n) break;
+          const float d = live ? dz[r][o + u * step] : 0.0f;
+          if (!live) break;
+#pragma unroll
+          for (int k = 0; k < kN; ++k) acc[r][k] = fmaf(d, a[u][k], acc[r][k]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    if (r >= n) break;
+    if (step > 1) {  // rows of threads, in their order
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kN; ++k) sums[threadIdx.x][k] = acc[r][k];
+      __syncthreads();
+      if (at == 0)
+        for (int y = 1; y < step; ++y)
+#pragma unroll
+          for (int k = 0; k < kN; ++k) acc[r][k] += sums[y * lanes + lane][k];
+    }
+    if (at != 0 || count <= 0) continue;
+    if (p.chunks > 1) store_values<float, false, kN>(p.parts + (((int64_t)chunk * p.M + q) * n + r) * p.n_in + col, count, acc[r]);
+    else store_values<T, false, kN>((T*)p.dx + q * p.dx_batch + r * p.dx_row + col, count, acc[r]);
+  }
+}
+template <typename T>
+__global__ __launch_bounds__(kElementThreads) void few_rows_total_kernel(const __grid_constant__ FewRowsBackParams p) {
+  ptx::let_successor_start();
+  ptx::wait_for_predecessor();
+  const int64_t row_length = p.n_in, each = (int64_t)p.n * row_length, total = each * p.M;
+  for (int64_t e = (int64_t)blockIdx.x * kElementThreads + threadIdx.x; e < total; e += (int64_t)gridDim.x * kElementThreads) {
+    float s = 0.0f;
+#pragma unroll 8
+    for (int c = 0; c < p.chunks; ++c) s += p.parts[c * total + e];
+    const int64_t q = e / each, r = (e - q * each) / row_length, col = e - q * each - r * row_length;
+    ((T*)p.dx)[q * p.dx_batch + r * p.dx_row + col] = (T)s;
+  }
+}
+
 }  // namespace netmax

@@ -456,6 +456,72 @@ int few_rows(Stream& s, const netmax_layer& l) {
   }
 }
 
+template <typename T, int kRows>
+int few_rows_backward(Stream& s, const netmax_layer& l, float* parts) {
+  constexpr int kN = 16 / sizeof(T);
+  FewRowsBackParams p;
+  const bool active = l.activation != NETMAX_ACTIVATION_NONE;
+  p.dy = l.dy.data;
+  p.dy_row = l.dy.row_stride;
+  p.dy_batch = l.dy.worker_stride;
+  if (active) {
+    p.z = l.z.data;
+    p.z_row = l.z.row_stride;
+    p.z_batch = l.z.worker_stride;
+  }
+  p.x = l.x.data;
+  p.x_row = l.x.row_stride;
+  p.x_batch = l.x.worker_stride;
+  p.weight = l.weight.data;
+  p.weight_row = l.weight.row_stride;
+  p.weight_batch = l.weight.worker_stride;
+  p.dx = l.dx.data;
+  p.dx_row = l.dx.row_stride;
+  p.dx_batch = l.dx.worker_stride;
+  p.dweight = l.dweight.data;
+  p.dweight_row = l.dweight.row_stride;
+  p.dweight_batch = l.dweight.worker_stride;
+  p.dbias = l.dbias.data;
+  p.dbias_batch = l.dbias.worker_stride;
+  p.M = l.M;
+  p.n = (int32_t)l.n;
+  p.n_in = (int32_t)l.n_in;
+  p.n_out = (int32_t)l.n_out;
+  p.activation = l.activation;
+  p.error = s.error;
+  while (p.shift < 8 && ((int64_t)kN << p.shift) < l.n_in) ++p.shift;
+  const int64_t tiles = ceil_div<int64_t>(l.n_in, (int64_t)kN << p.shift);
+  p.col_tiles = (int32_t)tiles;
+  if (l.dweight.data || l.dbias.data) {
+    const int64_t columns = l.dweight.data ? tiles : 1;
+    p.col_tiles = (int32_t)columns;
+    const int64_t blocks = columns * ceil_div<int64_t>(l.n_out, kFewOutputs);
+    if (blocks >= (int64_t)1 << 31) return fail_op(NETMAX_INVALID_ARG, "the layer's gradient has too many parts");
+    p.clear_error = s.clear;
+    s.clear = false;
+    OP_DO(launch(s, few_rows_dweight_kernel<T, kRows>, dim3((unsigned)blocks, (unsigned)l.M), kElementThreads, 0, 1, p));
+    p.col_tiles = (int32_t)tiles;
+  }
+  if (l.dx.data) {
+    // outputs are shared out until every SM has two CTAs; 64 at least, so that the parts fit in the room for the laid out weights
+    int64_t per = ceil_div<int64_t>(l.n_out, kFewOutputs) * kFewOutputs;
+    while (per > kFewOutputs && tiles * l.M * ceil_div(l.n_out, per) < 2 * sm_count()) per = ceil_div<int64_t>(per / 2, kFewOutputs) * kFewOutputs;
+    p.outputs_per_block = (int32_t)per;
+    p.chunks = (int32_t)ceil_div(l.n_out, per);
+    p.parts = parts;
+    if (tiles * p.chunks >= (int64_t)1 << 31) return fail_op(NETMAX_INVALID_ARG, "the layer's gradient has too many parts");
+    p.clear_error = s.clear;
+    s.clear = false;
+    OP_DO(launch(s, few_rows_dx_kernel<T, kRows>, dim3((unsigned)(tiles * p.chunks), (unsigned)l.M), kElementThreads, 0, 1, p));
+    if (p.chunks > 1) {
+      const int64_t total = (int64_t)l.M * l.n * l.n_in;
+      OP_DO(launch(s, few_rows_total_kernel<T>, dim3((unsigned)std::min<int64_t>(ceil_div<int64_t>(total, kElementThreads), 4096)), kElementThreads, 0, 1, p));
+    }
+  }
+  if (s.clear) OP_CUDA(cudaMemsetAsync(l.workspace, 0, 4, s.stream));
+  return NETMAX_OK;
+}
+
 // One product of a launch: D[m][n] over k.
 void fill_product(ProductGroup& g, const Prepared& a, bool a_mn, const Prepared& b, bool b_mn, int64_t M, int64_t N, int64_t K) {
   g.M = (int32_t)M;
@@ -663,6 +729,11 @@ int netmax_layer_backward(const netmax_layer* l) try {
     return NETMAX_OK;
   }
   const bool f32 = l->storage == NETMAX_STORAGE_F32;
+  if (f32 && n <= kFewRowsF32)
+    return n <= 4 ? few_rows_backward<float, 4>(s, *l, (float*)room.weight.planes) : n <= 8 ? few_rows_backward<float, 8>(s, *l, (float*)room.weight.planes)
+                                                                                   : few_rows_backward<float, 16>(s, *l, (float*)room.weight.planes);
+  if (!f32 && n <= (l->dx.data && !aligned16(l->weight, l->M) ? kFewRowsBf16Laid : kFewRowsBf16))
+    return n <= 4 ? few_rows_backward<__nv_bfloat16, 4>(s, *l, (float*)room.weight.planes) : few_rows_backward<__nv_bfloat16, 8>(s, *l, (float*)room.weight.planes);
   OperandParams jobs;
   int n_jobs = 0;
   Prepared dz, w, x;
