@@ -58,24 +58,28 @@ __global__ __launch_bounds__(kElementThreads) void few_rows_kernel(const __grid_
     for (; k + kN <= p.n_in; k += 32 * kN) step(k, kN, std::true_type());
   }
   for (; k < p.n_in; k += 32 * kN) step(k, min(kN, p.n_in - k), std::false_type());
-  float mine = 0.0f;  // lane o * kRows + r has output `first + o` of row r
+#pragma unroll
+  for (int h = 0; h < kOutputs * kRows; h += 32) {
+  float mine = 0.0f;  // lane o * kRows + r - h has output `first + o` of row r
 #pragma unroll
   for (int o = 0; o < kOutputs; ++o)
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
+      if (o * kRows + r < h || o * kRows + r >= h + 32) continue;
       float s = sum[o][r];
 #pragma unroll
       for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
-      if (lane == o * kRows + r) mine = s;
+      if (lane == o * kRows + r - h) mine = s;
     }
-  const int o = first + lane / kRows;
-  if (lane >= kOutputs * kRows || o >= p.n_out || lane % kRows >= n) return;
-  const int64_t r = rows_before + lane % kRows;
+  const int e = h + lane, o = first + e / kRows;
+  if (e >= kOutputs * kRows || o >= p.n_out || e % kRows >= n) continue;
+  const int64_t r = rows_before + e % kRows;
   if (p.bias) mine += (float)((const T*)p.bias)[q * p.bias_batch + o];
   if (p.z) ((T*)p.z)[q * p.z_batch + r * p.z_row + o] = (T)mine;
   mine = activate(mine, p.activation);
   if (p.residual) mine += (float)((const T*)p.residual)[q * p.residual_batch + r * p.residual_row + o];
   ((T*)p.y)[q * p.y_batch + r * p.y_row + o] = (T)mine;
+  }
 }
 
 // ---- the gradient of such batches: bound by writing dW and reading W once ----------------------

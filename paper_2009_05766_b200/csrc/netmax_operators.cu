@@ -225,13 +225,17 @@ int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilog
   };
   // Columns of a pair's tile: 256 with one plane, 128 with two (and of narrow outputs; symmetric ones never have more columns than rows).
   auto pair_columns = [&](const ProductGroup& g) { return p.planes == 2 || (!g.symmetric && g.N <= 128) ? 128 : 256; };
-  int64_t pairs = 0, wide = 0;
+  int64_t pairs = 0, wide = 0, area = 0;
   for (int k = 0; k < p.groups; ++k) {
     const ProductGroup& g = p.group[k];
-    pairs += tiles_of(g, factors[k].batch, 256, pair_columns(g));
+    const int64_t n = tiles_of(g, factors[k].batch, 256, pair_columns(g));
+    pairs += n;
+    area += n * 256 * pair_columns(g);
     wide += tiles_of(g, factors[k].batch, 128, 128);
   }
-  const int ctas = pairs * 5 >= sms / 2 * 4 ? 2 : 1;
+  // pairs where they keep four fifths of the SMs busy and cover not much more than tiles of 128 x 128 would (32 rows of 8 workers' fp32
+  // 4096 x 4096 layers: 187 us with half of every pair's tile empty, 105 so)
+  const int ctas = pairs * 5 >= sms / 2 * 4 && area * 2 <= wide * 128 * 128 * 3 ? 2 : 1;
   int64_t tiles = 0;
   int most_b = 0;
   for (int k = 0; k < p.groups; ++k) {
@@ -279,7 +283,8 @@ bool aligned16(const netmax_view& v, int count) {
 struct Prepared {
   Operand operand;
   bool batched = true;
-  int32_t* exponent = nullptr;
+  int32_t* exponent = nullptr;  // of each matrix, or of each row
+  bool by_rows = false;
 };
 
 Sweep make_sweep(int count, int64_t rows, int64_t cols) {
@@ -312,7 +317,7 @@ OperandRoom take_operand(Carver& c, int count, int64_t rows, int64_t cols, int s
   if (storage == NETMAX_STORAGE_F32) {
     // (a shared matrix is swept as one, in up to as many blocks as all of them)
     r.maxima = (float*)c.take(std::max((size_t)count * blocks_of(make_sweep(count, rows, cols)), (size_t)blocks_of(make_sweep(1, rows, cols))) * sizeof(float));
-    r.exponent = (int32_t*)c.take((size_t)count * sizeof(int32_t));
+    r.exponent = (int32_t*)c.take((size_t)count * (size_t)rows * sizeof(int32_t));
   }
   return r;
 }
@@ -347,7 +352,7 @@ void fill_source(OperandJob& j, const netmax_view& v, const netmax_view* z, int 
 
 // Either the view itself, where the tensor cores can read it, or a job that lays it out.
 Prepared prepare_operand(const netmax_view& v, const netmax_view* z, int activation, int count, int64_t rows, int64_t cols, int storage, const OperandRoom& room,
-                         OperandParams& jobs, int& n_jobs) {
+                         OperandParams& jobs, int& n_jobs, bool by_rows = false) {
   Prepared r;
   const bool shared = v.worker_stride == 0 && (!z || z->worker_stride == 0);
   const int matrices = shared ? 1 : count;
@@ -377,7 +382,25 @@ Prepared prepare_operand(const netmax_view& v, const netmax_view* z, int activat
   o.plane = j.dst_plane;
   o.planes = o.bf16 ? 1 : 2;
   r.exponent = room.exponent;
+  r.by_rows = by_rows && !o.bf16;
   return r;
+}
+
+// fp32 operands whose rows have exponents of their own.
+int run_row_jobs(Stream& s, OperandParams& jobs, int n_jobs) {
+  int count = 1, rows = 1;
+  for (int k = 0; k < n_jobs; ++k) {
+    count = std::max(count, jobs.job[k].sweep.count);
+    rows = std::max(rows, jobs.job[k].sweep.rows);
+  }
+  jobs.error = s.error;
+  jobs.clear_error = s.clear;
+  s.clear = false;
+  const int64_t cols = jobs.job[0].sweep.cols;
+  const int lanes = cols <= 1024 ? 32 : cols <= 2048 ? 64 : cols <= 4096 ? 128 : 256;
+  const dim3 grid((unsigned)ceil_div(rows, kElementThreads / lanes), (unsigned)std::min(count, 32768), (unsigned)n_jobs);
+  return launch(s, lanes == 32 ? operand_rows_kernel<32> : lanes == 64 ? operand_rows_kernel<64> : lanes == 128 ? operand_rows_kernel<128> : operand_rows_kernel<256>,
+                grid, kElementThreads, 0, 1, jobs);
 }
 
 int run_jobs(Stream& s, OperandParams& jobs, int n_jobs, int storage) {
@@ -533,6 +556,8 @@ void fill_product(ProductGroup& g, const Prepared& a, bool a_mn, const Prepared&
   g.b_batched = b.batched;
   g.exp_a = a.exponent;
   g.exp_b = b.exponent;
+  g.exp_a_rows = a.by_rows ? (int32_t)M : 0;
+  g.exp_b_rows = b.by_rows ? (int32_t)N : 0;
 }
 
 // ---- checks ---------------------------------------------------------------------------------------
@@ -659,9 +684,11 @@ int netmax_layer_forward(const netmax_layer* l) try {
   if (n <= (f32 ? kFewRowsF32 : aligned16(l->weight, l->M) ? kFewRowsBf16 : kFewRowsBf16Laid)) return few_rows(s, *l);
   OperandParams jobs;
   int n_jobs = 0;
-  const Prepared w = prepare_operand(l->weight, nullptr, 0, l->M, n_out, n_in, l->storage, room.weight, jobs, n_jobs);
-  const Prepared x = prepare_operand(l->x, nullptr, 0, l->M, n, n_in, l->storage, room.x, jobs, n_jobs);
-  OP_DO(run_jobs(s, jobs, n_jobs, l->storage));
+  // (both factors' rows end in the output, so each row has a scale of its own and the values are read once from memory)
+  const Prepared w = prepare_operand(l->weight, nullptr, 0, l->M, n_out, n_in, l->storage, room.weight, jobs, n_jobs, true);
+  const Prepared x = prepare_operand(l->x, nullptr, 0, l->M, n, n_in, l->storage, room.x, jobs, n_jobs, true);
+  if (f32) OP_DO(run_row_jobs(s, jobs, n_jobs));
+  else OP_DO(run_jobs(s, jobs, n_jobs, l->storage));
   ProductParams p;
   p.groups = 1;
   p.planes = l->storage == NETMAX_STORAGE_F32 ? 2 : 1;

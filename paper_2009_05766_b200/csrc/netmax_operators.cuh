@@ -237,6 +237,91 @@ __global__ __launch_bounds__(kElementThreads) void operand_kernel(const __grid_c
   }
 }
 
+// fp32 rows as two fp16 planes, each row times a power of two of its own.  kLanes threads a row, as many as hold it with up to
+// 32 values each in registers; rows longer than 8,192 are read again from L2.
+template <int kLanes>
+__global__ __launch_bounds__(kElementThreads) void operand_rows_kernel(const __grid_constant__ OperandParams p) {
+  constexpr int kHeld = 4;  // groups of eight values
+  ptx::let_successor_start();
+  ptx::wait_for_predecessor();
+  if (p.clear_error && blockIdx.x + blockIdx.y + blockIdx.z == 0 && threadIdx.x == 0) *p.error = 0;
+  const OperandJob j = p.job[blockIdx.z];
+  const int asked = blockIdx.x * (kElementThreads / kLanes) + threadIdx.x / kLanes, lane = threadIdx.x % kLanes, cols = j.sweep.cols;
+  if (blockIdx.x * (kElementThreads / kLanes) >= j.sweep.rows) return;
+  const bool live = asked < j.sweep.rows;  // (rows past the last one go through its motions, up to the stores)
+  const int row = live ? asked : j.sweep.rows - 1;
+  __shared__ float parts[kElementThreads / 32];
+  for (int q = blockIdx.y; q < j.sweep.count; q += gridDim.y) {
+    const float* src = (const float*)j.src + q * j.batch + row * j.row;
+    const int whole = ((uintptr_t)src & 15) == 0 ? cols / 8 * 8 : 0;  // columns that go in 16-byte pieces
+    float most = 0.0f, held[kHeld][8];
+    auto look = [&](float v) {
+      v = fabsf(v);
+      if (v <= 3.402823466e38f) most = fmaxf(most, v);
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int c = (i * kLanes + lane) * 8;
+      if (c >= whole) break;
+      load_values<float, true, 8>(src + c, 8, held[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      if ((i * kLanes + lane) * 8 >= whole) break;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) look(held[i][k]);
+    }
+    for (int c = (kHeld * kLanes + lane) * 8; c < whole; c += kLanes * 8) {
+      float v[8];
+      load_values<float, true, 8>(src + c, 8, v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) look(v[k]);
+    }
+    for (int c = whole + lane; c < cols; c += kLanes) look(src[c]);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+    if (kLanes > 32) {
+      __syncthreads();
+      if (threadIdx.x % 32 == 0) parts[threadIdx.x / 32] = most;
+      __syncthreads();
+      const int first = threadIdx.x / kLanes * (kLanes / 32);
+#pragma unroll
+      for (int w = 0; w < kLanes / 32; ++w) most = fmaxf(most, parts[first + w]);
+    }
+    if (!live) continue;
+    const int exponent = most > 0.0f ? min(14 - ilogbf(most), 126) : 0;
+    if (lane == 0) j.exponent[(int64_t)q * j.sweep.rows + row] = exponent;
+    const float scale = ldexpf(1.0f, exponent);
+    __half* dst = (__half*)j.dst + q * j.dst_batch + row * j.dst_row;
+    auto put = [&](int c, float (&v)[8]) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] *= scale;
+      uint4 hi, lo;
+      split8(v, hi, lo);
+      *(uint4*)(dst + c) = hi;
+      *(uint4*)(dst + c + j.dst_plane) = lo;
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int c = (i * kLanes + lane) * 8;
+      if (c >= whole) break;
+      put(c, held[i]);
+    }
+    for (int c = (kHeld * kLanes + lane) * 8; c < whole; c += kLanes * 8) {
+      float v[8];
+      load_values<float, true, 8>(src + c, 8, v);
+      put(c, v);
+    }
+    for (int c = whole + lane; c < cols; c += kLanes) {
+      const float v[4] = {src[c] * scale, 0.0f, 0.0f, 0.0f};
+      uint32_t hi[2], lo[2];
+      split_values<4>(v, hi, lo);
+      dst[c] = __ushort_as_half((unsigned short)hi[0]);
+      dst[c + j.dst_plane] = __ushort_as_half((unsigned short)lo[0]);
+    }
+  }
+}
+
 // The blocks' column sums added up, in double.
 template <typename T>
 __global__ __launch_bounds__(kElementThreads) void column_totals_kernel(const float* parts, int n_parts, int cols, int count, T* out, int64_t batch) {

@@ -77,7 +77,8 @@ struct ProductGroup {
   const void* residual = nullptr;  // or the planes of A (kPolynomial) and X (kUpdate, kLast*, kStep*)
   int64_t residual_row = 0, residual_batch = 0, residual_plane = 0;
   int32_t activation = 0;
-  const int32_t *exp_a = nullptr, *exp_b = nullptr;  // per matrix: its planes hold 2^exp times the values
+  const int32_t *exp_a = nullptr, *exp_b = nullptr;  // planes hold 2^exp times the values: per matrix, or per row of it
+  int32_t exp_a_rows = 0, exp_b_rows = 0;            // rows of a matrix that have exponents of their own; 0: per matrix
   int32_t first_matrix = 0;                          // of the step's table
   int32_t pieces = 0;                                // every row of every view above starts on a 16-byte boundary, and N is a multiple of 8
 };
@@ -451,9 +452,21 @@ struct LayerRows {
       : out(g.out_row), z(g.z_row), residual(g.residual_row), has_z(g.z != nullptr), has_residual(g.residual != nullptr), has_bias(g.bias != nullptr),
         activation(g.activation) {}
 };
+// 2^e for e in [-126, 127].
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
+// v 2^e for e in [-252, 252], in two factors, so that neither leaves fp32's range.
+__device__ __forceinline__ float times_power(float v, int e) { return v * power_of_two(e >> 1) * power_of_two(e - (e >> 1)); }
+// The exponents of rows and columns of a chunk, NULL where the whole matrix has one.
+struct Exponents {
+  const int32_t *rows = nullptr, *columns = nullptr;
+  __device__ __forceinline__ Exponents(const ProductGroup& g, int q) {
+    if (g.exp_a_rows) rows = g.exp_a + (int64_t)(g.a_batched ? q : 0) * g.exp_a_rows;
+    if (g.exp_b_rows) columns = g.exp_b + (int64_t)(g.b_batched ? q : 0) * g.exp_b_rows;
+  }
+};
 // y and z of a chunk whose 32 x 32 elements all exist, in 16-byte pieces.
 template <typename T>
-__device__ __forceinline__ void layer_chunk(const ProductGroup& g, int q, int m0, int n0, float f0, float f1, const float* slot) {
+__device__ __forceinline__ void layer_chunk(const ProductGroup& g, int q, int m0, int n0, int exponent, const float* slot) {
   constexpr int kN = sizeof(T) == 4 ? 4 : 8, kLanes = 32 / kN;
   const int lane = threadIdx.x % 32, c = lane % kLanes, n = n0 + kN * c, row = lane / kLanes;
   const LayerRows g1(g);
@@ -462,6 +475,14 @@ __device__ __forceinline__ void layer_chunk(const ProductGroup& g, int q, int m0
     const T* b = (const T*)g.bias + q * g.bias_batch + n;
 #pragma unroll
     for (int k = 0; k < kN; ++k) bias[k] = (float)b[k];
+  }
+  int column_exponent[kN], row_exponent[32 / kN];
+  if (sizeof(T) == 4) {
+    const Exponents e(g, q);
+#pragma unroll
+    for (int k = 0; k < kN; ++k) column_exponent[k] = exponent - (e.columns ? e.columns[n + k] : 0);
+#pragma unroll
+    for (int i = 0; i < 32 / kN; ++i) row_exponent[i] = e.rows ? e.rows[m0 + row + kN * i] : 0;
   }
   const T* r = (const T*)g.residual + q * g.residual_batch + (int64_t)(m0 + row) * g1.residual + n;
   T* z = (T*)g.z + q * g.z_batch + (int64_t)(m0 + row) * g1.z + n;
@@ -473,7 +494,7 @@ __device__ __forceinline__ void layer_chunk(const ProductGroup& g, int q, int m0
     read_slot(slot, kN * i + row, c, v);
     if (sizeof(T) == 4) {
 #pragma unroll
-      for (int k = 0; k < kN; ++k) v[k] = v[k] * f0 * f1;
+      for (int k = 0; k < kN; ++k) v[k] = times_power(v[k], column_exponent[k] - row_exponent[i]);
     }
     if (g1.has_bias) {
 #pragma unroll
@@ -490,10 +511,12 @@ __device__ __forceinline__ void layer_chunk(const ProductGroup& g, int q, int m0
 }
 // Of any chunk: a column a lane, so that a row's elements still go out together whatever their alignment.
 template <typename T>
-__device__ __forceinline__ void ragged_layer_chunk(const ProductGroup& g, int q, int m0, int n0, float f0, float f1, const float* slot) {
+__device__ __forceinline__ void ragged_layer_chunk(const ProductGroup& g, int q, int m0, int n0, int exponent, const float* slot) {
   const int lane = threadIdx.x % 32, n = n0 + lane, rows = n < g.N ? min(32, g.M - m0) : 0;
   const LayerRows g1(g);
   const float bias = g1.has_bias && rows > 0 ? (float)((const T*)g.bias)[q * g.bias_batch + n] : 0.0f;
+  const Exponents e(g, q);
+  if (sizeof(T) == 4 && e.columns && rows > 0) exponent -= e.columns[n];
   const T* r = (const T*)g.residual + q * g.residual_batch + (int64_t)m0 * g1.residual + n;
   T* z = (T*)g.z + q * g.z_batch + (int64_t)m0 * g1.z + n;
   T* y = (T*)g.out + q * g.out_batch + (int64_t)m0 * g1.out + n;
@@ -504,7 +527,7 @@ __device__ __forceinline__ void ragged_layer_chunk(const ProductGroup& g, int q,
     for (int u = 0; u < 8; ++u) {
       const int i = i0 + u;
       v[u] = slot[i * 32 + ((lane / 4) ^ (i & 7)) * 4 + lane % 4];
-      if (sizeof(T) == 4) v[u] = v[u] * f0 * f1;
+      if (sizeof(T) == 4) v[u] = times_power(v[u], exponent - (e.rows && i < rows ? e.rows[m0 + i] : 0));
       v[u] += bias;
     }
     if (g1.has_residual) {
@@ -592,10 +615,8 @@ __device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const Pro
   __syncwarp();
   if (kEpilogue == kLayerF32 || kEpilogue == kLayerBf16) {
     using T = typename std::conditional<kEpilogue == kLayerF32, float, __nv_bfloat16>::type;
-    // 2^exponent as two factors, so that neither leaves fp32's range
-    const float f0 = ldexpf(1.0f, exponent / 2), f1 = ldexpf(1.0f, exponent - exponent / 2);
-    if (g.pieces && m0 + 32 <= g.M && n0 + 32 <= g.N) layer_chunk<T>(g, t.q, m0, n0, f0, f1, slot);
-    else ragged_layer_chunk<T>(g, t.q, m0, n0, f0, f1, slot);
+    if (g.pieces && m0 + 32 <= g.M && n0 + 32 <= g.N) layer_chunk<T>(g, t.q, m0, n0, exponent, slot);
+    else ragged_layer_chunk<T>(g, t.q, m0, n0, exponent, slot);
     return;
   }
   if (kEpilogue == kStepF32 || kEpilogue == kStepBf16) {
@@ -806,7 +827,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
       const int m0 = (tile.i * kCtas + (int)rank) * 128 + (int)quadrant * 32, n0 = tile.j * g.bn;
       const int columns = m0 < g.M ? min(g.bn, g.N - n0) : 0;
       int exponent = 0;
-      if (kEpilogue == kLayerF32) exponent = -(g.exp_a[g.a_batched ? tile.q : 0] + g.exp_b[g.b_batched ? tile.q : 0]);
+      if (kEpilogue == kLayerF32) exponent = -((g.exp_a_rows ? 0 : g.exp_a[g.a_batched ? tile.q : 0]) + (g.exp_b_rows ? 0 : g.exp_b[g.b_batched ? tile.q : 0]));
       const int steps = (g.K + 63) / 64, per_part = kPlanes == 2 ? kPromote : steps;
       Residual<lane_columns(kEpilogue)> residual;
       if ((int)column < columns) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + column, lane, residual);
