@@ -451,13 +451,14 @@ int netmax_launch_shape(netmax_ctx* ctx, int64_t n_rounds, netmax_shape* out);
  * worker i is data[i * worker_stride + r * row_stride + c], strides in elements.  Inputs may overlap and repeat (worker_stride = 0
  * gives every worker the same matrix); the matrices of an output must not overlap each other or any input, except
  * that y may be the residual itself (the same address and strides).  Elements that no view names are left as they are.
- * Products are summed in fp32.  fp32 operands enter them as two fp16 parts scaled by a power of two per matrix (22 bits below the
- * matrix's largest finite magnitude); bfloat16 operands enter as they are.  Every other step is fp32, rounded once when it is
+ * Products are summed in fp32.  fp32 operands of large products enter them as two fp16 parts scaled by a power of two (22 bits, and no
+ * less than 2^-38 of the largest finite magnitude: of a row in netmax_layer_forward, of a matrix in netmax_layer_backward); bfloat16
+ * operands enter as they are, but for dz with an activation, which is rounded to bfloat16 first.  Every other step is fp32, rounded once when it is
  * stored.  An infinity or NaN among the inputs makes the outputs that depend on it infinite or NaN.
  *
  * `workspace` is device memory, 256-byte aligned, of the size that the matching call returns.  Calls that share one must run one
  * after the other (two captured graphs that share one, too).  Nothing is allocated and nothing waits for the device, so all of these
- * can be captured in a graph.  Every wait inside the kernels is bounded; netmax_workspace_status says whether one ran out.
+ * can be captured in a graph, but for netmax_round_orthogonalised, which moves its context on as netmax_round does.  Every wait inside the kernels is bounded; netmax_workspace_status says whether one ran out.
  */
 typedef struct netmax_view {
   void* data;            /* device; not written where the view is an input */

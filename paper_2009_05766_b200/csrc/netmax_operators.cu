@@ -276,8 +276,10 @@ int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilog
 }
 
 // ---- operands ---------------------------------------------------------------------------------
-bool aligned16(const netmax_view& v, int count) {
-  return ((uintptr_t)v.data & 15) == 0 && v.row_stride % 8 == 0 && (count == 1 || (v.worker_stride > 0 && v.worker_stride % 8 == 0));
+// Whether the tensor cores can read a view of 16-bit values in place: every row on a 16-byte boundary, matrices behind one another.
+bool in_place(const netmax_view& v, int count, int64_t rows, int64_t cols) {
+  if (((uintptr_t)v.data & 15) != 0 || (rows > 1 && v.row_stride % 8 != 0)) return false;
+  return count == 1 || (v.worker_stride % 8 == 0 && v.worker_stride >= (rows - 1) * v.row_stride + cols);
 }
 
 struct Prepared {
@@ -362,9 +364,9 @@ Prepared prepare_operand(const netmax_view& v, const netmax_view* z, int activat
   o.inner = cols;
   o.outer = rows;
   o.count = matrices;
-  if (o.bf16 && !z && aligned16(v, matrices)) {
+  if (o.bf16 && !z && in_place(v, matrices, rows, cols)) {
     o.data = v.data;
-    o.row = v.row_stride;
+    o.row = rows > 1 ? v.row_stride : up8(cols);
     o.batch = v.worker_stride;
     return r;
   }
@@ -681,7 +683,7 @@ int netmax_layer_forward(const netmax_layer* l) try {
     return NETMAX_OK;
   }
   const bool f32 = l->storage == NETMAX_STORAGE_F32;
-  if (n <= (f32 ? kFewRowsF32 : aligned16(l->weight, l->M) ? kFewRowsBf16 : kFewRowsBf16Laid)) return few_rows(s, *l);
+  if (n <= (f32 ? kFewRowsF32 : in_place(l->weight, l->M, n_out, n_in) ? kFewRowsBf16 : kFewRowsBf16Laid)) return few_rows(s, *l);
   OperandParams jobs;
   int n_jobs = 0;
   // (both factors' rows end in the output, so each row has a scale of its own and the values are read once from memory)
@@ -759,7 +761,7 @@ int netmax_layer_backward(const netmax_layer* l) try {
   if (f32 && n <= kFewRowsF32)
     return n <= 4 ? few_rows_backward<float, 4>(s, *l, (float*)room.weight.planes) : n <= 8 ? few_rows_backward<float, 8>(s, *l, (float*)room.weight.planes)
                                                                                    : few_rows_backward<float, 16>(s, *l, (float*)room.weight.planes);
-  if (!f32 && n <= (l->dx.data && !aligned16(l->weight, l->M) ? kFewRowsBf16Laid : kFewRowsBf16))
+  if (!f32 && n <= (l->dx.data && !in_place(l->weight, l->M, n_out, n_in) ? kFewRowsBf16Laid : kFewRowsBf16))
     return n <= 4 ? few_rows_backward<__nv_bfloat16, 4>(s, *l, (float*)room.weight.planes) : few_rows_backward<__nv_bfloat16, 8>(s, *l, (float*)room.weight.planes);
   OperandParams jobs;
   int n_jobs = 0;
@@ -1142,10 +1144,10 @@ int check_step(const netmax_step& t) {
   OP_DO(check_steps(t.steps));
   if (!std::isfinite(t.lr) || !std::isfinite(t.mu) || !std::isfinite(t.decay)) return fail_op(NETMAX_INVALID_ARG, "lr, mu and decay must be finite");
   const size_t size = element_size(t.storage);
-  OP_DO(check_view("x", t.x, t.M, 1, t.d, true, size));
+  OP_DO(check_view("x", t.x, t.M, 1, t.d, false, size));
   OP_DO(check_view("x_next", t.x_next, t.M, 1, t.d, true, size));
   OP_DO(check_view("gradient", t.gradient, t.M, 1, t.d, false, size));
-  OP_DO(check_view("momentum", t.momentum, t.M, 1, t.d, true, 4));
+  OP_DO(check_view("momentum", t.momentum, t.M, 1, t.d, false, 4));
   OP_DO(check_view("momentum_next", t.momentum_next, t.M, 1, t.d, true, 4));
   if (!t.peers || !t.weights) return fail_op(NETMAX_INVALID_ARG, "peers or weights is NULL");
   const Span x = span_of(t.x, t.M, 1, t.d, size), next = span_of(t.x_next, t.M, 1, t.d, size), g = span_of(t.gradient, t.M, 1, t.d, size),

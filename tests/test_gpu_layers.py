@@ -125,3 +125,167 @@ def test_backward(nm, size, storage):
         want = dz.sum(1)
         off = (n + 4) * 2.0 ** -24 * dz.abs().sum(1) + slope.sum(1)
         check(db, want, off + rounded(want.abs() + off, storage), f"dbias {name}")
+
+
+def forward(nm, x, w, **kw):
+    storage = "f32" if x.dtype == torch.float32 else "bf16"
+    M, n, n_in = x.shape
+    y = torch.full((M, n, w.shape[1]), float("nan"), dtype=x.dtype, device="cuda")
+    ws = workspace(nm, M, n, n_in, w.shape[1], storage)
+    nm.netmax_layer_forward(x, w, y, workspace=ws, **kw)
+    nm.netmax_workspace_status(ws)
+    return y
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [3, 40, 150])
+def test_views(nm, storage, n):
+    """Weights inside replicas, workers woven into one another, odd offsets, one matrix for all: the results of dense copies, bit for bit
+    where the same path is taken, and nothing outside the outputs written."""
+    t, M, n_in, n_out = TYPES[storage], 5, 72, 88
+    dense_x, dense_w, dense_dy = normal(1, M, n, n_in, dtype=t), normal(2, M, n_out, n_in, dtype=t), normal(3, M, n, n_out, dtype=t)
+
+    def embed(v, kind):
+        M, r, c = v.shape
+        if kind == "replica":       # behind 3 elements of a row as long as the matrix and 13 more
+            base = torch.full((M, r * c + 16), 7.0, dtype=t, device="cuda")
+            view = base.as_strided((M, r, c), (r * c + 16, c, 1), 3)
+        elif kind == "woven":
+            base = torch.full((r, M, c), 7.0, dtype=t, device="cuda")
+            view = base.transpose(0, 1)
+        else:
+            base = torch.full((M, r, c + 24), 7.0, dtype=t, device="cuda")
+            view = base[:, :, 8:8 + c]
+        view.copy_(v)
+        return base, view
+
+    want_y, want_z = torch.empty(M, n, n_out, dtype=t, device="cuda"), torch.empty(M, n, n_out, dtype=t, device="cuda")
+    ws = workspace(nm, M, n, n_in, n_out, storage)
+    nm.netmax_layer_forward(dense_x, dense_w, want_y, z=want_z, activation="silu", workspace=ws)
+    want_dx, want_dw, want_db = torch.empty_like(dense_x), torch.empty_like(dense_w), torch.empty(M, n_out, dtype=t, device="cuda")
+    nm.netmax_layer_backward(dense_dy, dense_x, dense_w, dx=want_dx, dweight=want_dw, dbias=want_db, z=want_z, activation="silu", workspace=ws)
+    unit = 2.0 ** -7 if storage == "bf16" else 2.0 ** -18
+    near = lambda got, want: ((got.double() - want.double()).norm() <= unit * want.double().norm()).item()  # noqa: E731
+    for kind in ("replica", "woven", "padded"):
+        (_, x), (_, w), (_, dy) = embed(dense_x, kind), embed(dense_w, kind), embed(dense_dy, kind)
+        (by, y), (bz, z) = embed(torch.zeros_like(want_y), kind), embed(torch.zeros_like(want_z), kind)
+        nm.netmax_layer_forward(x, w, y, z=z, activation="silu", workspace=ws)
+        assert near(y, want_y) and near(z, want_z), kind
+        (bx, dx), (bw, dw) = embed(torch.zeros_like(dense_x), kind), embed(torch.zeros_like(dense_w), kind)
+        bb = torch.full((M, n_out + 5), 7.0, dtype=t, device="cuda")
+        z.copy_(want_z)
+        nm.netmax_layer_backward(dy, x, w, dx=dx, dweight=dw, dbias=bb[:, 2:2 + n_out], z=z, activation="silu", workspace=ws)
+        nm.netmax_workspace_status(ws)
+        assert near(dx, want_dx) and near(dw, want_dw) and near(bb[:, 2:2 + n_out], want_db), kind
+        assert (bb[:, :2] == 7).all() and (bb[:, 2 + n_out:] == 7).all()
+        for base, view in ((by, y), (bz, z), (bx, dx), (bw, dw)):
+            view.fill_(7.0)
+            assert (base == 7).all(), kind      # (what was outside the view still is as it was)
+    one = dense_x[:1].expand(M, n, n_in)
+    assert near(forward(nm, one, dense_w), forward(nm, one.contiguous(), dense_w))
+    same = dense_w[:1].expand(M, n_out, n_in)
+    assert near(forward(nm, dense_x, same), forward(nm, dense_x, same.contiguous()))
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [2, 60, 300])
+def test_the_residual_as_the_output(nm, storage, n):
+    t = TYPES[storage]
+    x, w, r = normal(1, 3, n, 64, dtype=t), normal(2, 3, 96, 64, dtype=t), normal(3, 3, n, 96, dtype=t)
+    want = torch.empty_like(r)
+    ws = workspace(nm, 3, n, 64, 96, storage)
+    nm.netmax_layer_forward(x, w, want, residual=r, activation="gelu", workspace=ws)
+    nm.netmax_layer_forward(x, w, r, residual=r, activation="gelu", workspace=ws)
+    assert torch.equal(r, want)
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+def test_no_rows(nm, storage):
+    t = TYPES[storage]
+    w = normal(2, 3, 9, 7, dtype=t)
+    x, y = torch.empty(3, 0, 7, dtype=t, device="cuda"), torch.empty(3, 0, 9, dtype=t, device="cuda")
+    ws = workspace(nm, 3, 0, 7, 9, storage)
+    nm.netmax_layer_forward(x, w, y, workspace=ws)
+    dw, db = torch.full((3, 9, 12), 5.0, dtype=t, device="cuda"), torch.full((3, 9), 5.0, dtype=t, device="cuda")
+    nm.netmax_layer_backward(y, x, w, dweight=dw[:, :, 2:9], dbias=db, workspace=ws)
+    nm.netmax_workspace_status(ws)
+    assert (dw[:, :, 2:9] == 0).all() and (dw[:, :, :2] == 5).all() and (dw[:, :, 9:] == 5).all() and (db == 0).all()
+
+
+@pytest.mark.parametrize("n", [2, 50, 200])
+def test_each_row_for_itself(nm, n):
+    """fp32: rows of x and of the weights from 1e-18 to 1e18 in one call are each as exact as alone; a row with a NaN or an infinity makes
+    nothing else other than finite."""
+    x, w = normal(1, 2, n, 70), normal(2, 2, 90, 70)
+    a = 10.0 ** torch.linspace(-18, 18, n).cuda().float()
+    b = 10.0 ** torch.linspace(18, -18, 90).cuda().float()
+    xs, wsd = x * a[None, :, None], w * b[None, :, None]
+    y = forward(nm, xs, wsd).double()
+    want = xs.double() @ wsd.double().mT
+    bound = (2.0 ** -21 + (70 / 16 + 4) * 2.0 ** -23) * (xs.double().abs() @ wsd.double().abs().mT) + 2.0 ** -34 * 70 * xs.double().abs().amax(2)[:, :, None] * wsd.double().abs().amax(2)[:, None]
+    assert ((y - want).abs() <= bound + 2.0 ** -23 * want.abs()).all()
+    bad = x.clone()
+    bad[0, 1, 3], bad[1, 0, 5] = float("nan"), float("inf")
+    y, clean = forward(nm, bad, w), forward(nm, x, w)
+    assert not torch.isfinite(y[0, 1]).any() and not torch.isfinite(y[1, 0]).any()
+    y[0, 1], y[1, 0] = clean[0, 1], clean[1, 0]
+    assert torch.equal(y, clean)
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [3, 200])
+def test_in_a_graph_and_on_another_stream(nm, storage, n):
+    t, M, n_in, n_out = TYPES[storage], 4, 96, 160
+    x, w, dy = normal(1, M, n, n_in, dtype=t), normal(2, M, n_out, n_in, dtype=t), normal(3, M, n, n_out, dtype=t)
+    y, z = torch.empty(M, n, n_out, dtype=t, device="cuda"), torch.empty(M, n, n_out, dtype=t, device="cuda")
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(M, n_out, dtype=t, device="cuda")
+    ws = workspace(nm, M, n, n_in, n_out, storage)
+
+    def run(stream):
+        nm.netmax_layer_forward(x, w, y, z=z, activation="gelu", workspace=ws, stream=stream)
+        nm.netmax_layer_backward(dy, x, w, dx=dx, dweight=dw, dbias=db, z=z, activation="gelu", workspace=ws, stream=stream)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    run(side.cuda_stream)
+    side.synchronize()
+    first = [v.clone() for v in (y, dx, dw, db)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(torch.cuda.current_stream().cuda_stream)
+    for v in (y, z, dx, dw, db):
+        v.zero_()
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    for got, want in zip((y, dx, dw, db), first):
+        assert torch.equal(got, want)
+
+
+def test_two_streams_at_once(nm):
+    """Calls with workspaces of their own on two streams, products in pairs of CTAs beside clusters and small matrices."""
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    x, w = normal(1, 8, 700, 320), normal(2, 8, 640, 320)
+    u, v = normal(3, 12, 60, 1500), normal(4, 40, 64, 64)
+    y, ou, ov = torch.empty(8, 700, 640, device="cuda"), torch.empty_like(u), torch.empty_like(v)
+    wy = workspace(nm, 8, 700, 320, 640, "f32")
+    wu = torch.empty(nm.netmax_orthogonalise_workspace_size(12, 60, 1500), dtype=torch.uint8, device="cuda")
+    wv = torch.empty(nm.netmax_orthogonalise_workspace_size(40, 64, 64), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    nm.netmax_layer_forward(x, w, y, workspace=wy)
+    nm.netmax_orthogonalise(u, ou, workspace=wu)
+    nm.netmax_orthogonalise(v, ov, workspace=wv)
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (y, ou, ov)]
+    for t in (y, ou, ov):
+        t.zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        nm.netmax_layer_forward(x, w, y, workspace=wy, stream=a.cuda_stream)
+        nm.netmax_orthogonalise(u, ou, workspace=wu, stream=b.cuda_stream)
+        nm.netmax_orthogonalise(v, ov, workspace=wv, stream=b.cuda_stream)
+    torch.cuda.synchronize()
+    for ws in (wy, wu, wv):
+        nm.netmax_workspace_status(ws)
+    for got, w_ in zip((y, ou, ov), want):
+        assert torch.equal(got, w_)

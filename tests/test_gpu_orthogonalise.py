@@ -318,6 +318,30 @@ def test_a_round_after_a_capture_and_refusals_leave_the_context_as_it_was(nm):
     g.close()
 
 
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+def test_step_in_a_graph_and_from_one_replica(nm, storage):
+    M, d, matrices = 4, 150001, [(5, 64, 64, 1.0), (4101, 300, 400, 1.0), (124101, 60, 420, 1.0)]
+    x, m, grad, peers, weights = step_case(11, M, d, matrices, storage)
+    ws = torch.empty(nm.netmax_orthogonalised_step_workspace_size(M, d, matrices, storage), dtype=torch.uint8, device="cuda")
+    table = nm.matrix_table(matrices)
+    one = x[:1].expand(M, d)
+    for source in (x, one):
+        new, m_next, again, m_again = torch.empty_like(x), torch.empty_like(m), torch.empty_like(x), torch.empty_like(m)
+        nm.netmax_orthogonalised_step(source, new, grad, m, m_next, table, peers, weights, lr=0.1, workspace=ws)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            nm.netmax_orthogonalised_step(source, again, grad, m, m_again, table, peers, weights, lr=0.1, workspace=ws, stream=torch.cuda.current_stream().cuda_stream)
+        graph.replay()
+        graph.replay()
+        torch.cuda.synchronize()
+        nm.netmax_workspace_status(ws)
+        assert torch.equal(new, again) and torch.equal(m_next, m_again)
+    dense = torch.empty_like(x)
+    nm.netmax_orthogonalised_step(one.contiguous(), dense, grad, m, m_next, table, peers, weights, lr=0.1, workspace=ws)
+    assert torch.equal(dense, new)
+
+
 # ---- a run of all of them together
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])

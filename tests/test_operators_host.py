@@ -67,6 +67,7 @@ def test_what_is_allowed_reaches_the_device():
         assert code_of(b.lib().netmax_layer_backward, layer(**changes)) == -4
     assert code_of(b.lib().netmax_orthogonalise, orthogonal()) == -4
     assert code_of(b.lib().netmax_orthogonalised_step, step()) == -4
+    assert code_of(b.lib().netmax_orthogonalised_step, step(x=view(0, 1000, 0), momentum=view(3, 1000, 0))) == -4     # all workers from one replica
 
 
 def orthogonal(**changes):
