@@ -198,6 +198,7 @@ ProductKernel pick_product(int epilogue, int planes) {
     case kLastF32: return product_kernel<kCtas, kLastF32, 2>;
     case kLastBf16: return product_kernel<kCtas, kLastBf16, 1>;
     case kStepF32: return product_kernel<kCtas, kStepF32, 2>;
+    case kPartial: return planes == 2 ? product_kernel<kCtas, kPartial, 2> : product_kernel<kCtas, kPartial, 1>;
     default: return product_kernel<kCtas, kStepBf16, 1>;
   }
 }
@@ -206,6 +207,8 @@ ProductKernel pick_product(int epilogue, int planes) {
 struct Factors {
   const Operand *a = nullptr, *b = nullptr;
   int batch = 0;
+  float* parts = nullptr;  // kGram: room for the sums over parts of k, most_splits of them
+  int64_t most_splits = 1;
 };
 
 // Chooses the tile shape for all groups of a launch and runs it.
@@ -235,8 +238,12 @@ int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilog
   }
   // pairs where they keep four fifths of the SMs busy and cover not much more than tiles of 128 x 128 would (32 rows of 8 workers' fp32
   // 4096 x 4096 layers: 187 us with half of every pair's tile empty, 105 so)
-  const int ctas = pairs * 5 >= sms / 2 * 4 && area * 2 <= wide * 128 * 128 * 3 ? 2 : 1;
-  int64_t tiles = 0;
+  int ctas = pairs * 5 >= sms / 2 * 4 && area * 2 <= wide * 128 * 128 * 3 ? 2 : 1;
+  if (epilogue == kGram && p.groups == 1 && factors[0].parts && ctas == 1 && area * 2 <= wide * 128 * 128 * 3) {
+    const int64_t most = std::min<int64_t>(factors[0].most_splits, ceil_div(p.group[0].K, 64) / 8);
+    if (pairs * most * 5 >= sms / 2 * 4) ctas = 2;  // in parts of k: see below
+  }
+  int64_t tiles = 0, combine_blocks = 0;
   int most_b = 0;
   for (int k = 0; k < p.groups; ++k) {
     ProductGroup& g = p.group[k];
@@ -257,6 +264,43 @@ int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilog
     most_b = std::max(most_b, g.bn / ctas);
   }
   if (tiles == 0) return NETMAX_OK;
+  // Few tiles with long sums: several CTAs (or pairs) add up parts of k, and a launch behind them the parts.  At least eight steps of 64 k
+  // a part.
+  CombineParams combine;
+  if (epilogue == kGram && tiles * 2 <= sms / ctas) {
+    const int64_t share = sms / ctas / tiles;
+    bool split = false;
+    tiles = 0;
+    for (int k = 0; k < p.groups; ++k) {
+      ProductGroup& g = p.group[k];
+      const int64_t all = ceil_div(g.K, 64), want = factors[k].parts ? std::min({share, factors[k].most_splits, all / 8}) : 1;
+      g.splits = want > 1 ? (int)ceil_div(all, ceil_div(all, want)) : 1;  // (every part has steps)
+      split = split || g.splits > 1;
+      g.tile_begin = (int)tiles;
+      tiles += tiles_of(g, factors[k].batch * g.splits, 128 * ctas, g.bn);
+    }
+    int64_t blocks = 0;
+    for (int k = 0; split && k < p.groups; ++k) {
+      ProductGroup& g = p.group[k];
+      CombineGroup& c = combine.group[k];
+      c.parts = factors[k].parts;
+      c.out = (__half*)g.out;
+      c.row = g.out_row;
+      c.part_batch = c.out_batch = g.out_batch;
+      c.out_plane = g.out_plane;
+      c.side = g.M;
+      c.splits = g.splits;
+      c.batch = factors[k].batch;
+      c.first_block = (int)blocks;
+      const int64_t edge = ceil_div(g.M, 32);
+      blocks += c.batch * (edge * (edge + 1) / 2);
+      g.out = factors[k].parts;
+      combine.groups = k + 1;
+    }
+    if (split) epilogue = kPartial;
+    combine.planes = p.planes;
+    combine_blocks = blocks;
+  }
   if (tiles > (int64_t)1 << 30) return fail_op(NETMAX_INVALID_ARG, "the problem has %lld tiles, more than 2^30", (long long)tiles);
   p.tiles = (int)tiles;
   p.a_bytes = 128 * 128;
@@ -272,6 +316,7 @@ int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilog
   const int grid = (int)std::min<int64_t>(tiles, sms / ctas) * ctas;
   OP_DO(launch(s, kernel, dim3(grid), kProductThreads, smem, ctas, p));
   s.clear = false;
+  if (combine_blocks > 0) OP_DO(launch(s, combine_kernel, dim3((unsigned)combine_blocks), kElementThreads, 0, 1, combine));
   return NETMAX_OK;
 }
 
@@ -897,6 +942,10 @@ int run_schulz(Stream& s, std::vector<SchulzGroup>& groups, int steps, int plane
             g.K = (int32_t)(phase == 0 && !q.tall ? q.cols : phase == 0 ? q.rows : q.side);
             g.a_mn = g.b_mn = phase == 0 && q.tall;
             factors[k].a = factors[k].b = phase == 0 ? &q.op_x[now] : &q.op_gram;
+            if (phase == 0) {  // (the other iterate is written behind the polynomial only)
+              factors[k].parts = (float*)q.x[now ^ 1];
+              factors[k].most_splits = q.x_batch / q.s_batch;  // fp32 parts in the room of two planes
+            }
             g.out = phase == 0 ? q.gram : q.poly;
             g.out_row = q.s_row;
             g.out_batch = q.s_batch;

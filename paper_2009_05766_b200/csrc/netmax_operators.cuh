@@ -406,6 +406,63 @@ __global__ __launch_bounds__(kElementThreads) void first_iterate_kernel(const __
   }
 }
 
+// S from its parts: the 32 x 32 blocks on and below the diagonal, added up in the parts' order, as planes, the others mirrored.
+struct CombineGroup {
+  const float* parts = nullptr;  // [matrix][split][side][row]
+  __half* out = nullptr;
+  int64_t row = 0, part_batch = 0, out_batch = 0, out_plane = 0;
+  int32_t side = 0, splits = 1, batch = 0, first_block = 0;  // blocks of all its matrices, from first_block on
+};
+struct CombineParams {
+  CombineGroup group[kMaxGroups];
+  int32_t groups = 0, planes = 1;
+};
+__global__ __launch_bounds__(kElementThreads) void combine_kernel(const __grid_constant__ CombineParams p) {
+  __shared__ uint32_t turned[32][33];
+  ptx::let_successor_start();
+  ptx::wait_for_predecessor();
+  int k = 0;
+  while (k + 1 < p.groups && p.group[k + 1].first_block <= (int)blockIdx.x) ++k;
+  const CombineGroup g = p.group[k];
+  const int edge = (g.side + 31) / 32, per = edge * (edge + 1) / 2;
+  int t = (int)blockIdx.x - g.first_block;
+  const int q = t / per;
+  t -= q * per;
+  int i = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+  while (i * (i + 1) / 2 > t) --i;
+  while ((i + 1) * (i + 2) / 2 <= t) ++i;
+  const int j = t - i * (i + 1) / 2, r = threadIdx.x / 8, c = threadIdx.x % 8 * 4, m = i * 32 + r, n = j * 32 + c;
+  uint32_t hi[2] = {}, lo[2] = {};
+  const bool live = m < g.side && n < g.side;
+  if (live) {
+    float v[4] = {};
+    const float* at = g.parts + (int64_t)q * g.splits * g.part_batch + (int64_t)m * g.row + n;
+    for (int s = 0; s < g.splits; ++s) {
+      const float4 a = *(const float4*)(at + s * g.part_batch);
+      v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] *= kPlaneUnscale;
+    split_values<4>(v, hi, lo);
+    __half* out = g.out + q * g.out_batch + (int64_t)m * g.row + n;
+    store_words(out, hi);
+    if (p.planes == 2) store_words(out + g.out_plane, lo);
+  }
+  if (i == j) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) turned[c + e][r] = (hi[e / 2] >> (16 * (e % 2)) & 0xFFFF) | (lo[e / 2] >> (16 * (e % 2))) << 16;
+  __syncthreads();
+  const int m2 = j * 32 + r, n2 = i * 32 + c;
+  if (m2 >= g.side || n2 >= g.side) return;
+  uint32_t w[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = turned[r][c + e];
+  const uint32_t h[2] = {__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410)}, l[2] = {__byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632)};
+  __half* out = g.out + q * g.out_batch + (int64_t)m2 * g.row + n2;
+  store_words(out, h);
+  if (p.planes == 2) store_words(out + g.out_plane, l);
+}
+
 // ---- the step: momentum, norms, and everything that no matrix covers ---------------------------
 struct StepSegment {
   uint32_t first_piece, offset, length;

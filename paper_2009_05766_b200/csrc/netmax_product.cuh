@@ -55,6 +55,7 @@ enum Epilogue {
   kUpdate,                // planes of a X + D, X from planes
   kLastF32, kLastBf16,    // the same, out as fp32 / bf16
   kStepF32, kStepBf16,    // the same, into a worker's local step and its pull
+  kPartial,               // D over a part of k, as fp32 (symmetric; combine_kernel adds the parts up)
 };
 
 struct ProductGroup {
@@ -64,6 +65,7 @@ struct ProductGroup {
   int32_t symmetric = 0;       // only tiles up to the diagonal, the others mirrored: a tile's rows over its columns (1 or 2); 0: no
   int32_t a_mn = 0, b_mn = 0;  // m (n) contiguous instead of k
   int32_t a_box = 64, b_box = 64;  // rows of a box
+  int32_t splits = 1;          // parts of k, each with a tile of its own
   int32_t bn = 0;              // columns of a tile
   int32_t a_batched = 1, b_batched = 1;  // 0: one matrix for all
   uint32_t idesc = 0;
@@ -247,7 +249,7 @@ __device__ __forceinline__ float activation_slope(float z, int activation) {
 }
 
 struct Tile {
-  int g, q, i, j;  // group, matrix, tile row (m) and column (n)
+  int g, q, s, i, j;  // group, matrix, part of k, tile row (m) and column (n)
 };
 __device__ __forceinline__ Tile find_tile(const ProductParams& p, int t) {
   Tile out;
@@ -271,7 +273,15 @@ __device__ __forceinline__ Tile find_tile(const ProductParams& p, int t) {
     out.j = t / g.tiles_m;
     out.i = t - out.j * g.tiles_m;
   }
+  out.s = out.q % g.splits;
+  out.q /= g.splits;
   return out;
+}
+// The steps of 64 k of a tile's part.
+__device__ __forceinline__ int first_step(const ProductGroup& g, const Tile& t) { return t.s * (((g.K + 63) / 64 + g.splits - 1) / g.splits); }
+__device__ __forceinline__ int steps_of(const ProductGroup& g, const Tile& t) {
+  const int all = (g.K + 63) / 64, per = (all + g.splits - 1) / g.splits;
+  return min(per, all - t.s * per);
 }
 
 // Two or four words of packed 16-bit values.
@@ -385,7 +395,7 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo
 }
 // Columns that a lane takes of a row of a staged chunk: eight where 16-bit values are stored, four where fp32 is (16 bytes either way;
 // with eight, two stores would each fill halves of their sectors).  32 / kN lanes a row, kN rows at a time, 32 / kN times.
-__host__ __device__ constexpr int lane_columns(int epilogue) { return epilogue == kLayerF32 || epilogue == kLastF32 || epilogue == kStepF32 ? 4 : 8; }
+__host__ __device__ constexpr int lane_columns(int epilogue) { return epilogue == kLayerF32 || epilogue == kLastF32 || epilogue == kStepF32 || epilogue == kPartial ? 4 : 8; }
 
 // What an epilogue reads besides the accumulator, both planes, as it will go over the chunk.
 template <int kN>
@@ -628,6 +638,17 @@ __device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const Pro
   const int c = lane % kLanes, n = n0 + kN * c, row = lane / kLanes, count = min(kN, g.N - n), rows = count > 0 ? g.M - m0 - row : 0;
   const int64_t out_step = kN * g.out_row, out_plane = g.out_plane;  // (in registers: see LayerRows)
   const float ca = p.ca, cb = p.cb, cc = p.cc;
+  if (kEpilogue == kPartial) {
+    float* out = (float*)g.out + (int64_t)(t.q * g.splits + t.s) * g.out_batch + (int64_t)(m0 + row) * g.out_row + n;
+#pragma unroll
+    for (int i = 0; i < 32 / kN; ++i, out += out_step) {
+      if (kN * i >= rows) break;
+      float v[kN];
+      read_slot(slot, kN * i + row, c, v);
+      store_values<float, true>(out, kN, v);  // (rows are padded to eight columns)
+    }
+    return;
+  }
   if (kEpilogue == kLastF32 || kEpilogue == kLastBf16) {
     using T = typename std::conditional<kEpilogue == kLastF32, float, __nv_bfloat16>::type;
     T* out = (T*)g.out + t.q * g.out_batch + (int64_t)(m0 + row) * g.out_row + n;
@@ -756,7 +777,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
       const int qa = g.a_batched ? tile.q : 0, qb = g.b_batched ? tile.q : 0;
       const int boxes_b = rows_b / kProductBox;
       const uint32_t bytes = (uint32_t)(kPlanes * (2 + boxes_b) * kBoxBytes) * kCtas;
-      const int steps = (g.K + 63) / 64;
+      const int steps = steps_of(g, tile), before = first_step(g, tile);
       for (int kb = 0; kb < steps; ++kb, ++issued) {
         const int s = issued % p.stages, lap = issued / p.stages;
         if (lap > 0 && !ptx::wait(empty + 8 * s, (lap - 1) & 1)) { ok = false; break; }
@@ -766,10 +787,10 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
         const uint32_t at = base + s * p.stage_bytes;
         for (int plane = 0; plane < kPlanes; ++plane) {
           for (int b = 0; b < 2; b += g.a_box / 64)
-            ptx::load_box<kCtas>(at + plane * p.a_bytes + b * kBoxBytes, &g.a, bar, g.a_mn ? m0 + 64 * b : kb * 64, g.a_mn ? kb * 64 : m0 + 64 * b, qa, plane);
+            ptx::load_box<kCtas>(at + plane * p.a_bytes + b * kBoxBytes, &g.a, bar, g.a_mn ? m0 + 64 * b : (before + kb) * 64, g.a_mn ? (before + kb) * 64 : m0 + 64 * b, qa, plane);
           for (int b = 0; b < boxes_b; b += g.b_box / 64)
-            ptx::load_box<kCtas>(at + kPlanes * p.a_bytes + plane * p.b_bytes + b * kBoxBytes, &g.b, bar, g.b_mn ? n0 + 64 * b : kb * 64,
-                                 g.b_mn ? kb * 64 : n0 + 64 * b, qb, plane);
+            ptx::load_box<kCtas>(at + kPlanes * p.a_bytes + plane * p.b_bytes + b * kBoxBytes, &g.b, bar, g.b_mn ? n0 + 64 * b : (before + kb) * 64,
+                                 g.b_mn ? (before + kb) * 64 : n0 + 64 * b, qb, plane);
         }
       }
     }
@@ -792,7 +813,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
       const uint32_t step_a = (g.a_mn ? 2048 : 32) >> 4, step_b = (g.b_mn ? 2048 : 32) >> 4;  // 16 k further
       const uint32_t low_a = ptx::descriptor_low(base, g.a_mn ? kBoxBytes : 16), low_b = ptx::descriptor_low(base + kPlanes * p.a_bytes, g.b_mn ? kBoxBytes : 16);
       const uint32_t plane_a = p.a_bytes >> 4, plane_b = p.b_bytes >> 4, stage_step = p.stage_bytes >> 4, idesc = g.idesc;
-      const int steps = (g.K + 63) / 64, per_part = kPlanes == 2 ? kPromote : steps;
+      const int steps = steps_of(g, tile), per_part = kPlanes == 2 ? kPromote : steps;
       for (int begin = 0; begin < steps && ok; begin += per_part, ++part) {
         const int acc = part % kAccumulators, lap = part / kAccumulators;
         if (lap > 0 && !ptx::wait(drained + 8 * acc, (lap - 1) & 1)) { ok = false; break; }
@@ -828,7 +849,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
       const int columns = m0 < g.M ? min(g.bn, g.N - n0) : 0;
       int exponent = 0;
       if (kEpilogue == kLayerF32) exponent = -((g.exp_a_rows ? 0 : g.exp_a[g.a_batched ? tile.q : 0]) + (g.exp_b_rows ? 0 : g.exp_b[g.b_batched ? tile.q : 0]));
-      const int steps = (g.K + 63) / 64, per_part = kPlanes == 2 ? kPromote : steps;
+      const int steps = steps_of(g, tile), per_part = kPlanes == 2 ? kPromote : steps;
       Residual<lane_columns(kEpilogue)> residual;
       if ((int)column < columns) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + column, lane, residual);
       float sum[32];

@@ -123,7 +123,8 @@ SIZES = [(1, 1, 1), (2, 1, 9), (2, 9, 1), (3, 5, 7), (4, 64, 64), (2, 64, 27), (
          (1, 129, 512), (2, 256, 256), (5, 257, 255), (2, 600, 520), (33, 40, 24), (1, 1003, 777), (2, 512, 1536), (3, 1100, 1100),
          (3, 27, 4024), (2, 3726, 11), (3, 97, 2513), (1, 128, 4096), (1, 8192, 64), (2, 64, 8191), (1, 8193, 64), (1, 128, 4097), (4, 64, 512), (40, 100, 256),
          (5, 65, 1025), (1, 1, 5000), (20, 31, 956), (7, 600, 128),
-         (75, 70, 300), (74, 300, 70)]
+         (75, 70, 300), (74, 300, 70),
+         (2, 200, 5000), (1, 5001, 300), (3, 513, 2100), (1, 140, 9000)]
 
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
