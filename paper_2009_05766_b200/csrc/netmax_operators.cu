@@ -237,7 +237,7 @@ int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilog
     wide += tiles_of(g, factors[k].batch, 128, 128);
   }
   // pairs where they keep four fifths of the SMs busy and cover not much more than tiles of 128 x 128 would (32 rows of 8 workers' fp32
-  // 4096 x 4096 layers: 187 us with half of every pair's tile empty, 105 so)
+  // 4096 x 4096 layers: the call takes 375 us with half of every pair's tile empty, 308 so)
   int ctas = pairs * 5 >= sms / 2 * 4 && area * 2 <= wide * 128 * 128 * 3 ? 2 : 1;
   if (epilogue == kGram && p.groups == 1 && factors[0].parts && ctas == 1 && area * 2 <= wide * 128 * 128 * 3) {
     const int64_t most = std::min<int64_t>(factors[0].most_splits, ceil_div(p.group[0].K, 64) / 8);
@@ -290,10 +290,9 @@ int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilog
       c.out_plane = g.out_plane;
       c.side = g.M;
       c.splits = g.splits;
-      c.batch = factors[k].batch;
       c.first_block = (int)blocks;
       const int64_t edge = ceil_div(g.M, 32);
-      blocks += c.batch * (edge * (edge + 1) / 2);
+      blocks += factors[k].batch * (edge * (edge + 1) / 2);
       g.out = factors[k].parts;
       combine.groups = k + 1;
     }
@@ -681,12 +680,12 @@ int check_apart(const char* name, const Span& out, const char* other, const Span
 
 extern "C" {
 
-int netmax_layer_workspace_size(int32_t M, int64_t n, int64_t n_in, int64_t n_out, int32_t storage, size_t* bytes) {
+int netmax_layer_workspace_size(int32_t M, int64_t n, int64_t n_in, int64_t n_out, int32_t storage, size_t* bytes) try {
   OP_DO(check_layer_sizes(M, n, n_in, n_out, storage));
   if (!bytes) return fail_op(NETMAX_INVALID_ARG, "bytes is NULL");
   *bytes = layer_room(nullptr, M, n, n_in, n_out, storage).total;
   return NETMAX_OK;
-}
+} NM_CATCH(fail_caught)
 
 int netmax_layer_forward(const netmax_layer* l) try {
   if (!l) return fail_op(NETMAX_INVALID_ARG, "layer is NULL");
@@ -1030,12 +1029,12 @@ int check_steps(int steps) {
 
 extern "C" {
 
-int netmax_orthogonalise_workspace_size(int32_t count, int64_t rows, int64_t cols, int32_t storage, size_t* bytes) {
+int netmax_orthogonalise_workspace_size(int32_t count, int64_t rows, int64_t cols, int32_t storage, size_t* bytes) try {
   OP_DO(check_orthogonal_sizes(count, rows, cols, storage));
   if (!bytes) return fail_op(NETMAX_INVALID_ARG, "bytes is NULL");
   *bytes = orthogonal_room(nullptr, count, rows, cols, storage).total;
   return NETMAX_OK;
-}
+} NM_CATCH(fail_caught)
 
 int netmax_orthogonalise(const netmax_orthogonal* o) try {
   if (!o) return fail_op(NETMAX_INVALID_ARG, "o is NULL");
@@ -1095,7 +1094,7 @@ int netmax_orthogonalise(const netmax_orthogonal* o) try {
   });
 } NM_CATCH(fail_caught)
 
-int netmax_workspace_status(const void* workspace, int32_t device, void* stream) {
+int netmax_workspace_status(const void* workspace, int32_t device, void* stream) try {
   if (!workspace) return fail_op(NETMAX_INVALID_ARG, "workspace is NULL");
   OP_DO(check_device(device));
   OnDevice on(device);
@@ -1105,7 +1104,7 @@ int netmax_workspace_status(const void* workspace, int32_t device, void* stream)
   OP_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
   if (word) return fail_op(NETMAX_CUDA_ERROR, "a bounded wait inside a kernel ran out; the outputs of the last call that used this workspace are not to be used");
   return NETMAX_OK;
-}
+} NM_CATCH(fail_caught)
 
 }  // extern "C"
 

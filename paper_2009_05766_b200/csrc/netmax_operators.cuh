@@ -411,7 +411,7 @@ struct CombineGroup {
   const float* parts = nullptr;  // [matrix][split][side][row]
   __half* out = nullptr;
   int64_t row = 0, part_batch = 0, out_batch = 0, out_plane = 0;
-  int32_t side = 0, splits = 1, batch = 0, first_block = 0;  // blocks of all its matrices, from first_block on
+  int32_t side = 0, splits = 1, first_block = 0;  // blocks of all its matrices, from first_block on
 };
 struct CombineParams {
   CombineGroup group[kMaxGroups];

@@ -289,3 +289,36 @@ def test_two_streams_at_once(nm):
         nm.netmax_workspace_status(ws)
     for got, w_ in zip((y, ou, ov), want):
         assert torch.equal(got, w_)
+
+
+@pytest.mark.parametrize("n", [2, 12, 40])
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+def test_workers_further_apart_than_32_bits(nm, storage, n):
+    """Two workers' views 2^31 + 64 elements apart: every entry's offsets are 64 bits wide."""
+    t, n_in, n_out, apart = TYPES[storage], 40, 72, 2 ** 31 + 64
+    used = 3 * n * n_out + 2 * n * n_in + 2 * n_out * n_in  # of all views, x, w, z, y, dy, dx and dw, in one worker
+    room = torch.empty(apart + used, dtype=t, device="cuda")
+    at = 0
+    def far(seed, rows, cols):  # the two matrices of a view, each in its worker's part of the room
+        nonlocal at
+        v = room.as_strided((2, rows, cols), (apart, cols, 1), at)
+        at += rows * cols
+        if seed:
+            v.copy_(normal(seed, 2, rows, cols, dtype=t))
+        return v
+    x, w, z = far(1, n, n_in), far(2, n_out, n_in), far(0, n, n_out)
+    y = far(0, n, n_out)
+    ws = workspace(nm, 2, n, n_in, n_out, storage)
+    nm.netmax_layer_forward(x, w, y, z=z, activation="silu", workspace=ws)
+    nm.netmax_workspace_status(ws)
+    want = x.double() @ w.double().mT
+    off = product_bound(x, w, storage) + 2.0 ** -22 * want.abs()
+    check(z, want, off + rounded(want, storage), "z")
+    value = act(want, "silu")
+    check(y, value, 1.13 * off + 2.0 ** -20 * want.abs() + rounded(value.abs() + off, storage), "y")
+    dy, dx, dw = far(3, n, n_out), far(0, n, n_in), far(0, n_out, n_in)
+    nm.netmax_layer_backward(dy, x, w, dx=dx, dweight=dw, workspace=ws)
+    nm.netmax_workspace_status(ws)
+    for got, a, b, what in ((dx, dy, w.mT, "dx"), (dw, dy.mT, x.mT, "dw")):
+        true = a.double() @ b.mT.double()
+        check(got, true, product_bound(a, b, storage) + rounded(true, storage), what)

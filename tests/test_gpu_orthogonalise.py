@@ -407,3 +407,18 @@ def test_workers_train_a_network(nm, storage):
         got = torch.from_numpy(g.read_replicas()).cuda().double()
         assert ((got - new).abs() <= off + 2.0 ** -21 * new.abs()).all()
     g.close()
+
+
+@pytest.mark.parametrize("shape", [(40, 24), (130, 200)], ids=str)
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+def test_matrices_further_apart_than_32_bits(nm, storage, shape):
+    """Two matrices 2^31 + 64 elements apart, on both paths."""
+    t, (rows, cols), apart = {"f32": torch.float32, "bf16": torch.bfloat16}[storage], shape, 2 ** 31 + 64
+    room = torch.empty(apart + 2 * rows * cols, dtype=t, device="cuda")
+    u = room.as_strided((2, rows, cols), (apart, cols, 1), 0)
+    out = room.as_strided((2, rows, cols), (apart, cols, 1), rows * cols)
+    u.copy_(update(5, 2, rows, cols, dtype=t))
+    ws = torch.full((nm.netmax_orthogonalise_workspace_size(2, rows, cols, storage),), 0x7F, dtype=torch.uint8, device="cuda")
+    nm.netmax_orthogonalise(u, out, workspace=ws)
+    nm.netmax_workspace_status(ws)
+    check(out, u)
