@@ -188,7 +188,10 @@ int launch(Stream& s, void (*kernel)(Params...), dim3 grid, int threads, size_t 
 
 using ProductKernel = void (*)(const ProductParams);
 template <int kCtas>
-ProductKernel pick_product(int epilogue, int planes) {
+ProductKernel pick_product(int epilogue, int planes, bool long_sums) {
+  if (long_sums)
+    return epilogue == kLayerBf16 ? product_kernel<kCtas, kLayerBf16, 1, true> : epilogue == kGram ? product_kernel<kCtas, kGram, 1, true>
+                                                                                                   : product_kernel<kCtas, kPartial, 1, true>;
   switch (epilogue) {
     case kLayerF32: return product_kernel<kCtas, kLayerF32, 2>;
     case kLayerBf16: return product_kernel<kCtas, kLayerBf16, 1>;
@@ -226,8 +229,10 @@ int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilog
     const int64_t tm = ceil_div(g.M, tile_m), tn = ceil_div(g.N, bn);
     return (int64_t)batch * (g.symmetric ? tile_m / bn * (tm * (tm - 1) / 2) + tn : tm * tn);
   };
-  // Columns of a pair's tile: 256 with one plane, 128 with two (and of narrow outputs; symmetric ones never have more columns than rows).
-  auto pair_columns = [&](const ProductGroup& g) { return p.planes == 2 || (!g.symmetric && g.N <= 128) ? 128 : 256; };
+  bool long_sums = false;  // (see kLongPart)
+  for (int k = 0; k < p.groups; ++k) long_sums = long_sums || (p.planes == 1 && (epilogue == kLayerBf16 || epilogue == kGram) && p.group[k].K > kLongPart * 64);
+  // Columns of a pair's tile: 256 with one plane, 128 with two and with long sums (and of narrow outputs; symmetric ones never have more columns than rows).
+  auto pair_columns = [&](const ProductGroup& g) { return p.planes == 2 || long_sums || (!g.symmetric && g.N <= 128) ? 128 : 256; };
   int64_t pairs = 0, wide = 0, area = 0;
   for (int k = 0; k < p.groups; ++k) {
     const ProductGroup& g = p.group[k];
@@ -310,7 +315,7 @@ int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilog
   const size_t smem = std::max(kLeastSmem, (size_t)1024 + slots + (size_t)p.stages * p.stage_bytes);
   p.error = s.error;
   p.clear_error = s.clear;
-  ProductKernel kernel = ctas == 2 ? pick_product<2>(epilogue, p.planes) : pick_product<1>(epilogue, p.planes);
+  ProductKernel kernel = ctas == 2 ? pick_product<2>(epilogue, p.planes, long_sums) : pick_product<1>(epilogue, p.planes, long_sums);
   OP_CUDA(raise_smem_limit((const void*)kernel, smem));
   const int grid = (int)std::min<int64_t>(tiles, sms / ctas) * ctas;
   OP_DO(launch(s, kernel, dim3(grid), kProductThreads, smem, ctas, p));

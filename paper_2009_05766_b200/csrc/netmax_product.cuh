@@ -723,10 +723,17 @@ __device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const Pro
 // every 256 k it is 8.4e-7 at any K (fp32 FMAs: 4.1e-7 at K = 512, 1.1e-6 at 4096), every 128 k 3.9e-7, but then the products wait for
 // accumulators (four layers of 2048 x 2048 x 2048: 183 us, 172 so, 168 without).
 constexpr int kPromote = 4;
+// One plane: products of up to 2^15 k stay in one accumulator.  What its 2^11 steps drop of a sum whose terms have one sign is then at most
+// 2^-12 of it, an eighth of bfloat16's rounding (sums of 2^23 positive products came out 5 % too small without a limit).  kLong has the epilogue add up parts
+// of that length, of tiles of up to 128 columns, so that every warp has one chunk of a tile.  Its instances are those whose k is a batch's rows, a layer's
+// inputs or outputs or a matrix's longer side; the others' k is a smaller side, at most 46,340.
+constexpr int kLongPart = 512;
 
-template <int kCtas, int kEpilogue, int kPlanes>
+template <int kCtas, int kEpilogue, int kPlanes, bool kLong = false>
 __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __grid_constant__ ProductParams p) {
+  static_assert(kPlanes == 1 || !kLong, "two planes have short parts anyway");
   constexpr int kLoader = kEpilogueWarps, kMultiplier = kEpilogueWarps + 1;
+  constexpr bool kParts = kPlanes == 2 || kLong;  // sums in registers, of one chunk a warp
   extern __shared__ unsigned char raw[];
   constexpr int kAccumulators = accumulators(kPlanes), kAccumulatorColumns = 512 / kAccumulators;
   __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 2 * kAccumulators];
@@ -813,7 +820,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
       const uint32_t step_a = (g.a_mn ? 2048 : 32) >> 4, step_b = (g.b_mn ? 2048 : 32) >> 4;  // 16 k further
       const uint32_t low_a = ptx::descriptor_low(base, g.a_mn ? kBoxBytes : 16), low_b = ptx::descriptor_low(base + kPlanes * p.a_bytes, g.b_mn ? kBoxBytes : 16);
       const uint32_t plane_a = p.a_bytes >> 4, plane_b = p.b_bytes >> 4, stage_step = p.stage_bytes >> 4, idesc = g.idesc;
-      const int steps = steps_of(g, tile), per_part = kPlanes == 2 ? kPromote : steps;
+      const int steps = steps_of(g, tile), per_part = kPlanes == 2 ? kPromote : kLong ? kLongPart : steps;
       for (int begin = 0; begin < steps && ok; begin += per_part, ++part) {
         const int acc = part % kAccumulators, lap = part / kAccumulators;
         if (lap > 0 && !ptx::wait(drained + 8 * acc, (lap - 1) & 1)) { ok = false; break; }
@@ -849,11 +856,11 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
       const int columns = m0 < g.M ? min(g.bn, g.N - n0) : 0;
       int exponent = 0;
       if (kEpilogue == kLayerF32) exponent = -((g.exp_a_rows ? 0 : g.exp_a[g.a_batched ? tile.q : 0]) + (g.exp_b_rows ? 0 : g.exp_b[g.b_batched ? tile.q : 0]));
-      const int steps = steps_of(g, tile), per_part = kPlanes == 2 ? kPromote : steps;
+      const int steps = steps_of(g, tile), per_part = kPlanes == 2 ? kPromote : kLong ? kLongPart : steps;
       Residual<lane_columns(kEpilogue)> residual;
       if ((int)column < columns) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + column, lane, residual);
       float sum[32];
-      if (kPlanes == 2) {
+      if (kParts) {
 #pragma unroll
         for (int c = 0; c < 32; ++c) sum[c] = 0.0f;
       }
@@ -866,7 +873,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
         }
         ptx::fence_after();
         const uint32_t from = tmem + (quadrant * 32 << 16) + acc * kAccumulatorColumns;
-        if (kPlanes == 2) {
+        if (kParts) {
           if ((int)column < columns) {
             float v[32];
             ptx::tmem_load32(from + column, v);
@@ -890,7 +897,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
           else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(drained + 8 * acc) : "memory");
         }
       }
-      if (kPlanes == 2 && ok && (int)column < columns) {
+      if (kParts && ok && (int)column < columns) {
         __syncwarp();
         stage_row(slot, sum);
         epilogue_chunk<kEpilogue, kPlanes>(p, g, tile, m0, n0 + column, exponent, slot, residual);
