@@ -569,7 +569,8 @@ typedef struct netmax_update {
   double mu, decay;
   int32_t nesterov;
   int32_t steps;
-  void* workspace;            /* of netmax_orthogonalised_step_workspace_size */
+  void* workspace;            /* of netmax_orthogonalised_step_workspace_size; like the others, used on the context's stream: what
+                                 they hold must be ready there */
   size_t workspace_bytes;
 } netmax_update;
 int netmax_round_orthogonalised(netmax_ctx* ctx, const netmax_update* update);
