@@ -449,8 +449,10 @@ int netmax_launch_shape(netmax_ctx* ctx, int64_t n_rounds, netmax_shape* out);
  *
  * All arrays are device memory of `storage`'s type (momentum: fp32 in both).  A netmax_view names M matrices: element (r, c) of
  * worker i is data[i * worker_stride + r * row_stride + c], strides in elements.  Inputs may overlap and repeat (worker_stride = 0
- * gives every worker the same matrix); the matrices of an output must not overlap each other or any input, except
- * that y may be the residual itself (the same address and strides).  Elements that no view names are left as they are.
+ * gives every worker the same matrix), but rows of one matrix may not (row_stride >= columns where there are several); the matrices of an
+ * output must not overlap each other, any input or another output, except that y may be the residual itself (the same address and strides).
+ * Views may lie between one another's rows and matrices where that shows from strides alone: side by side modulo the largest number that
+ * divides all strides of both, or, with equal worker strides, modulo those.  Other views whose ranges of addresses meet are refused.  Elements that no view names are left as they are.
  * Products are summed in fp32 (on the tensor cores in parts of up to 2^15 terms, each off by at most 2^-12 of the sum of its terms' magnitudes; parts of 256 with fp32 operands).  fp32 operands of large products enter them as two fp16 parts scaled by a power of two (22 bits, and no
  * less than 2^-38 of the largest finite magnitude: of a row in netmax_layer_forward, of a matrix in netmax_layer_backward); bfloat16
  * operands enter as they are, but for dz with an activation, which is rounded to bfloat16 first.  Every other step is fp32, rounded once when it is

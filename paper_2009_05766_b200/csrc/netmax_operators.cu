@@ -8,6 +8,7 @@
 #include <cstdio>
 #include <cstring>
 #include <mutex>
+#include <numeric>
 #include <tuple>
 #include <unordered_map>
 #include <vector>
@@ -660,17 +661,26 @@ int check_layer_sizes(int32_t M, int64_t n, int64_t n_in, int64_t n_out, int32_t
 }
 size_t element_size(int storage) { return storage == NETMAX_STORAGE_F32 ? 4 : 2; }
 
-// First and last byte of what a view names; of its matrices, how long each is and how far apart they stand.
+// First and last byte of what a view names; of its matrices, how long each is and how far apart they stand (0: there is one); of its rows,
+// how long each is and how far apart they stand (0: there is one).
 struct Span {
   uintptr_t first, last;
-  size_t extent, period;
+  size_t extent, period, width, row;
 };
 Span span_of(const netmax_view& v, int64_t count, int64_t rows, int64_t cols, size_t element) {
   const int64_t extent = (rows - 1) * v.row_stride + cols, end = (count - 1) * v.worker_stride + extent;
-  return {(uintptr_t)v.data, (uintptr_t)v.data + (size_t)end * element - 1, (size_t)extent * element, count > 1 ? (size_t)v.worker_stride * element : 0};
+  return {(uintptr_t)v.data, (uintptr_t)v.data + (size_t)end * element - 1, (size_t)extent * element, count > 1 ? (size_t)v.worker_stride * element : 0,
+          (size_t)cols * element, rows > 1 ? (size_t)v.row_stride * element : 0};
 }
 bool meet(const Span& a, const Span& b) {
   if (a.first > b.last || b.first > a.last) return false;
+  // Every row of either starts a multiple of the strides' common divisor behind the first one: columns of one wide buffer are apart if they
+  // are apart in that.
+  const size_t common = std::gcd(std::gcd(a.row, b.row), std::gcd(a.period, b.period));
+  if (common > 0) {
+    const size_t behind = b.first >= a.first ? (size_t)(b.first - a.first) % common : (common - (size_t)(a.first - b.first) % common) % common;
+    if (behind >= a.width && behind + b.width <= common) return false;
+  }
   if (a.period == 0 || a.period != b.period) return true;  // (woven in some other way: taken to overlap)
   // both once in every replica, as a layer's gradients are: apart if they are apart in one period
   const size_t between = (size_t)((b.first - a.first) % a.period + a.period) % a.period;

@@ -1,0 +1,87 @@
+"""More of what the operators on real weights accept and refuse, and rules of their sources that no run may be needed to see (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+from paper_2009_05766_b200 import binding as b
+
+BASE = 1 << 44      # an address that nothing is read from
+NONE = b.View(None, 0, 0)
+
+
+def no_gpu():
+    torch = pytest.importorskip("torch")
+    if torch.cuda.is_available():
+        pytest.skip("would run")
+
+
+# ---- views that lie between one another
+M, N, N_IN, N_OUT = 3, 20, 8, 16
+WIDE = 64     # columns of a buffer that x, y, z, the residual and dx share
+
+
+def layer(**changes):
+    ws = b.netmax_layer_workspace_size(M, N, N_IN, N_OUT)
+    far = lambda k, row, worker: b.View(BASE + (k << 36), row, worker)  # noqa: E731
+    a = b.Layer(M, N, N_IN, N_OUT, 0, 0, far(0, N_IN, N * N_IN), far(1, N_IN, N_IN * N_OUT), NONE, NONE, far(4, N_OUT, N * N_OUT), NONE,
+                far(6, N_OUT, N * N_OUT), NONE, NONE, NONE, 0, None, BASE + (20 << 36), ws)
+    for k, v in changes.items():
+        setattr(a, k, v)
+    return a
+
+
+def column(first, row=WIDE, worker=N * WIDE):
+    return b.View(BASE + 4 * first, row, worker)
+
+
+APART = [   # (changes of a forward call)
+    dict(x=column(0), y=column(8)),
+    dict(x=column(56), y=column(40)),
+    dict(x=column(0), y=column(8), z=column(24), residual=column(40)),
+    dict(M=1, x=column(0), y=column(8)),
+    dict(x=column(0, M * WIDE, WIDE), y=column(8, M * WIDE, WIDE)),                 # workers woven into one another
+    dict(x=column(0, WIDE, 0), y=column(8)),                                        # one input for all
+    dict(x=column(0, WIDE, WIDE), y=column(8, M * WIDE, WIDE)),                     # sliding windows beside woven outputs
+    dict(x=column(0, 2 * WIDE, 2 * N * WIDE), y=column(8)),                         # every second row
+    dict(n=1, x=column(0, 0, WIDE), y=column(8, 0, WIDE)),
+]
+OVERLAPPING = [
+    dict(x=column(0), y=column(7)),
+    dict(x=column(56), y=column(41)),
+    dict(x=column(0), y=column(49)),                                                # its last column is the next row's first
+    dict(M=1, x=column(0), y=column(7)),
+    dict(x=column(0, M * WIDE, WIDE), y=column(7, M * WIDE, WIDE)),
+    dict(x=column(0, WIDE, 0), y=column(7)),
+    dict(x=column(0), y=column(8), z=column(23)),
+    dict(x=column(0, WIDE - 8, N * (WIDE - 8)), y=column(8)),                       # rows that drift against one another
+    dict(n=1, x=column(0, 0, WIDE), y=column(7, 0, WIDE)),
+]
+
+
+@pytest.mark.parametrize("changes", APART)
+def test_disjoint_columns_are_no_overlap(changes):
+    no_gpu()
+    assert b.lib().netmax_layer_forward(C.addressof(layer(**changes))) == -4
+
+
+@pytest.mark.parametrize("changes", OVERLAPPING)
+def test_shared_columns_are_an_overlap(changes):
+    assert b.lib().netmax_layer_forward(C.addressof(layer(**changes))) == -1
+
+
+@pytest.mark.parametrize("changes,code", [(dict(x=column(0), dy=column(8), dx=column(24)), -4), (dict(x=column(0), dy=column(8), dx=column(23)), -1),
+                                          (dict(x=column(0), dy=column(8), dx=column(57), dweight=b.View(BASE + (8 << 36), N_IN, N_IN * N_OUT)), -1)])
+def test_disjoint_columns_of_a_gradient(changes, code):
+    if code == -4:
+        no_gpu()
+    assert b.lib().netmax_layer_backward(C.addressof(layer(**changes))) == code
+
+
+def test_matrices_between_one_another():
+    ws = b.netmax_orthogonalise_workspace_size(4, 20, 30)
+    for first, code in ((30, -4), (29, -1), (71, -1), (70, -4)):
+        if code == -4:
+            no_gpu()
+        a = b.Orthogonal(4, 20, 30, 0, 5, b.View(BASE, 100, 2000), b.View(BASE + 4 * first, 100, 2000), 0, None, BASE + (20 << 36), ws)
+        assert b.lib().netmax_orthogonalise(C.addressof(a)) == code, first
+
