@@ -456,7 +456,8 @@ int netmax_launch_shape(netmax_ctx* ctx, int64_t n_rounds, netmax_shape* out);
  * Products are summed in fp32 (on the tensor cores in parts of up to 2^15 terms, each off by at most 2^-12 of the sum of its terms' magnitudes; parts of 256 with fp32 operands).  fp32 operands of large products enter them as two fp16 parts scaled by a power of two (22 bits, and no
  * less than 2^-38 of the largest finite magnitude: of a row in netmax_layer_forward, of a matrix in netmax_layer_backward); bfloat16
  * operands enter as they are, but for dz with an activation, which is rounded to bfloat16 first.  Every other step is fp32, rounded once when it is
- * stored.  An infinity or NaN among the inputs makes the outputs that depend on it infinite or NaN.
+ * stored.  An infinity or NaN among the inputs makes the outputs that depend on it infinite or NaN (but relu takes -infinity to 0,
+ * and its slope at an infinite z is 0 or 1).
  *
  * `workspace` is device memory, 256-byte aligned, of the size that the matching call returns.  Calls that share one must run one
  * after the other (two captured graphs that share one, too).  Nothing is allocated and nothing waits for the device, so all of these

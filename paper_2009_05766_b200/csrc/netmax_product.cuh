@@ -238,7 +238,7 @@ __device__ __forceinline__ float activate(float z, int activation) {
   return z;
 }
 __device__ __forceinline__ float activation_slope(float z, int activation) {
-  if (activation == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
+  if (activation == kActRelu) return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);  // (NaN stays NaN)
   if (activation == kActGelu) {
     float e;
     const float p = gauss(z, e);

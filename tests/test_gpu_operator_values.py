@@ -34,6 +34,38 @@ def backward(nm, dy, x, w, z, activation):
     return dx, dw, db
 
 
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [3, 12, 90])
+@pytest.mark.parametrize("activation", ["none", "relu", "gelu", "silu"])
+def test_what_is_not_finite_spreads_as_far_as_it_counts(nm, activation, n, storage):
+    """A NaN or an infinity among dy, z, x or the weights makes those sums infinite or NaN that it enters, and leaves all others as they were.  (relu's
+    slope at an infinite z is 0 or 1.)"""
+    t, M, n_in, n_out, worker, row, out, col = TYPES[storage], 2, 70, 90, 1, 2, 17, 5
+    sources = {"dy": normal(1, M, n, n_out, dtype=t), "z": normal(2, M, n, n_out, dtype=t), "x": normal(3, M, n, n_in, dtype=t), "w": normal(4, M, n_out, n_in, dtype=t)}
+    places = {"dy": (worker, row, out), "z": (worker, row, out), "x": (worker, row, col), "w": (worker, out, col)}
+    for name, at in places.items():
+        sources[name][at] = 0.25        # (the largest of no matrix)
+    call = lambda s: backward(nm, s["dy"], s["x"], s["w"], s["z"], activation)  # noqa: E731
+    clean = call(sources)
+    for name, at in places.items():
+        for value in (float("nan"), float("inf"), float("-inf")):
+            if name == "z" and (activation == "none" or (activation == "relu" and value == value)):
+                continue
+            changed = dict(sources)
+            changed[name] = sources[name].clone()
+            changed[name][at] = value
+            touched = [torch.zeros_like(v, dtype=torch.bool) for v in clean]
+            if name in ("dy", "z"):
+                touched[0][worker, row] = touched[1][worker, out] = touched[2][worker, out] = True
+            elif name == "x":
+                touched[1][worker, :, col] = True
+            else:
+                touched[0][worker, :, col] = True
+            for got, want, where in zip(call(changed), clean, touched):
+                assert not torch.isfinite(got[where]).any(), (name, value)
+                assert torch.equal(got[~where], want[~where]), (name, value)
+
+
 @pytest.mark.parametrize("n", [12, 40, 300])
 def test_gradients_of_rows_of_different_size(nm, n):
     """fp32: rows of dy from 1 down to 2^-40.  Up to 16 rows every value counts in full; beyond, factors keep 22 bits and no less than 2^-38 of their
