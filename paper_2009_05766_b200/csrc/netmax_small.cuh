@@ -141,6 +141,12 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
   }
   if (warp == 0) ptx::tmem_alloc<1>(ptx::smem(&tmem_at), p.tmem_columns);
   for (uint32_t at = threadIdx.x * 16; at < 2 * x_plane; at += kSmallThreads * 16) *(uint4*)(x + at) = make_uint4(0, 0, 0, 0);
+  ptx::fence_before();
+  __syncthreads();
+  ptx::fence_after();
+  const uint32_t tmem = tmem_at;
+  // Only now that this CTA holds its TMEM: a CTA of the successor that takes an SM's columns first and waits for this grid, beside one of
+  // this grid that waits for columns, would never end.
   ptx::let_successor_start();
   if (!p.behind_rest) ptx::wait_for_predecessor();
   if (p.clear_error && blockIdx.x == 0 && threadIdx.x == 0) *p.error = 0;
@@ -176,10 +182,7 @@ __global__ __launch_bounds__(kSmallThreads, 1) void small_schulz_kernel(const __
 #pragma unroll
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
   if (lane == 0) squares[warp] = sum;
-  ptx::fence_before();
   __syncthreads();
-  ptx::fence_after();
-  const uint32_t tmem = tmem_at;
   sum = 0.0;
 #pragma unroll
   for (int w = 0; w < kSmallThreads / 32; ++w) sum += squares[w];

@@ -1,10 +1,14 @@
 """More of what the operators on real weights accept and refuse, and rules of their sources that no run may be needed to see (no GPU needed)."""
 import ctypes as C
+import os
+import re
 
 import pytest
 
 from paper_2009_05766_b200 import binding as b
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2009_05766_b200", "csrc")
 BASE = 1 << 44      # an address that nothing is read from
 NONE = b.View(None, 0, 0)
 
@@ -85,3 +89,19 @@ def test_matrices_between_one_another():
         a = b.Orthogonal(4, 20, 30, 0, 5, b.View(BASE, 100, 2000), b.View(BASE + 4 * first, 100, 2000), 0, None, BASE + (20 << 36), ws)
         assert b.lib().netmax_orthogonalise(C.addressof(a)) == code, first
 
+
+# ---- tensor memory
+def test_a_kernel_lets_its_successor_start_only_once_it_holds_its_tensor_memory():
+    """A CTA of the successor that takes an SM's tensor memory and waits for this grid, beside one of this grid that waits for tensor memory, would
+    never end.  So every kernel that allocates some reads the address behind a barrier before it lets its successor start."""
+    checked = 0
+    for name in sorted(os.listdir(CSRC)):
+        text = open(os.path.join(CSRC, name)).read()
+        for body in re.split(r"__global__", text)[1:]:
+            body = body.split("\n}\n")[0]
+            if "tmem_alloc<" not in body:
+                continue
+            checked += 1
+            alloc, read, start = (body.index(s) for s in ("tmem_alloc<", "= tmem_at;", "let_successor_start()"))
+            assert alloc < body.index("__syncthreads()", alloc) < read < start, name
+    assert checked == 2
