@@ -272,21 +272,21 @@ def _view(name, t, like, shape):
     return View(t.data_ptr(), row, strides[0] if shape[0] > 1 else max(1, rows) * row)
 
 
-def _device_of(t):
-    if t.device.type != "cuda":
-        raise ValueError(f"expected a CUDA tensor, got one on {t.device}")
-    return t.device.index or 0
-
-
-def _stream_of(t, stream):
-    """The stream that a call is given, or else torch's current one on its tensors' device (other arrays: the legacy default stream)."""
-    if stream is not None:
-        return stream
-    torch = sys.modules.get("torch")
-    if torch is None or not isinstance(t, torch.Tensor):
-        return None
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)     # (0.14 us; the public query makes an object: 2.2 of the smallest call's 11)
-    return raw(_device_of(t)) if raw is not None else torch.cuda.current_stream(t.device).cuda_stream
+def _place(t, stream):
+    """Device and stream of a call: the stream that it is given, or else torch's current one on its tensors' device (other arrays: the legacy
+    default stream)."""
+    device = t.device
+    if device.type != "cuda":
+        raise ValueError(f"expected a CUDA tensor, got one on {device}")
+    index = device.index or 0
+    if stream is None:
+        torch = sys.modules.get("torch")
+        if torch is not None and isinstance(t, torch.Tensor):
+            try:
+                stream = torch._C._cuda_getCurrentRawStream(index)      # (0.1 us; the public query makes an object: 2.2 of the smallest call's 11)
+            except AttributeError:
+                stream = torch.cuda.current_stream(device).cuda_stream
+    return index, stream
 
 
 def _workspace(t, like):
@@ -313,7 +313,7 @@ def netmax_layer_forward(x, weight, y, bias=None, residual=None, z=None, activat
     rows = (M, n, n_out)
     a = Layer(M, n, n_in, n_out, _storage_of(x), ACTIVATIONS[activation], _view("x", x, x, (M, n, n_in)),
               _view("weight", weight, x, (M, n_out, n_in)), _view("bias", bias, x, (M, n_out)), _view("residual", residual, x, rows),
-              _view("y", y, x, rows), _view("z", z, x, rows), _NO_VIEW, _NO_VIEW, _NO_VIEW, _NO_VIEW, _device_of(x), _stream_of(x, stream), ws, size)
+              _view("y", y, x, rows), _view("z", z, x, rows), _NO_VIEW, _NO_VIEW, _NO_VIEW, _NO_VIEW, *_place(x, stream), ws, size)
     code = lib().netmax_layer_forward(C.addressof(a))
     if code:
         _check(code)
@@ -328,7 +328,7 @@ def netmax_layer_backward(dy, x, weight, dx=None, dweight=None, dbias=None, z=No
     a = Layer(M, n, n_in, n_out, _storage_of(dy), ACTIVATIONS[activation], _view("x", x, dy, (M, n, n_in)),
               _view("weight", weight, dy, (M, n_out, n_in)), _NO_VIEW, _NO_VIEW, _NO_VIEW, _view("z", z, dy, (M, n, n_out)),
               _view("dy", dy, dy, (M, n, n_out)), _view("dx", dx, dy, (M, n, n_in)), _view("dweight", dweight, dy, (M, n_out, n_in)),
-              _view("dbias", dbias, dy, (M, n_out)), _device_of(dy), _stream_of(dy, stream), ws, size)
+              _view("dbias", dbias, dy, (M, n_out)), *_place(dy, stream), ws, size)
     code = lib().netmax_layer_backward(C.addressof(a))
     if code:
         _check(code)
@@ -345,7 +345,7 @@ def netmax_orthogonalise(u, out, steps: int = 5, workspace=None, stream: Optiona
     count, rows, cols = u.shape
     ws, size = _workspace(workspace, u)
     a = Orthogonal(count, rows, cols, _storage_of(u), int(steps), _view("u", u, u, (count, rows, cols)),
-                   _view("out", out, u, (count, rows, cols)), _device_of(u), _stream_of(u, stream), ws, size)
+                   _view("out", out, u, (count, rows, cols)), *_place(u, stream), ws, size)
     code = lib().netmax_orthogonalise(C.addressof(a))
     if code:
         _check(code)
@@ -378,7 +378,7 @@ def netmax_orthogonalised_step(x, x_next, gradient, momentum, momentum_next, mat
     a = Step(M, d, _storage_of(x), _view("x", x, x, (M, d)), _view("x_next", x_next, x, (M, d)), _view("gradient", gradient, x, (M, d)),
              _view("momentum", momentum, momentum, (M, d)), _view("momentum_next", momentum_next, momentum, (M, d)), C.addressof(table),
              len(table), peers.data_ptr(), weights.data_ptr(), float(lr), float(mu), float(decay), int(bool(nesterov)), int(steps),
-             _device_of(x), _stream_of(x, stream), ws, size)
+             *_place(x, stream), ws, size)
     code = lib().netmax_orthogonalised_step(C.addressof(a))
     if code:
         _check(code)
@@ -386,7 +386,7 @@ def netmax_orthogonalised_step(x, x_next, gradient, momentum, momentum_next, mat
 
 def netmax_workspace_status(workspace, stream: Optional[int] = None):
     """Waits for the stream; raises if a bounded wait ran out in the last call that used this workspace."""
-    _check(lib().netmax_workspace_status(workspace.data_ptr(), _device_of(workspace), _stream_of(workspace, stream)))
+    _check(lib().netmax_workspace_status(workspace.data_ptr(), *_place(workspace, stream)))
 
 
 class Netmax:
@@ -577,7 +577,7 @@ class Netmax:
             raise ValueError(f"gradient: expected {self.storage} values, got {gradient.dtype}")
         if str(momentum.dtype) != "torch.float32" or momentum.device != gradient.device:
             raise ValueError(f"momentum: expected torch.float32 on {gradient.device}, got {momentum.dtype} on {momentum.device}")
-        if _device_of(gradient) != self.device:
+        if _place(gradient, 0)[0] != self.device:
             raise ValueError(f"gradient: expected a tensor on device {self.device}, got one on {gradient.device}")
         g = _view("gradient", gradient, gradient, (self.M, self.d))
         m = _view("momentum", momentum, momentum, (self.M, self.d))
