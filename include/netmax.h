@@ -546,7 +546,7 @@ typedef struct netmax_step {
   int32_t n_matrices;
   const int32_t* peers;                       /* device, M */
   const float* weights;                       /* device, M */
-  double lr, mu, decay;                       /* used at their fp32 roundings */
+  double lr, mu, decay;                       /* used at their fp32 roundings, which must be finite (scale's too) */
   int32_t nesterov;
   int32_t steps;
   int32_t device;

@@ -1148,7 +1148,7 @@ int plan_step(int32_t M, int64_t d, const netmax_matrix* matrices, int32_t n, in
     if (m.rows < 1 || m.cols < 1 || m.offset < 0 || m.rows > d || m.cols > d || m.offset > d || m.rows * m.cols > d - m.offset)
       return fail_op(NETMAX_INVALID_ARG, "a matrix of %lld x %lld at %lld does not lie in a replica of %lld elements", (long long)m.rows, (long long)m.cols,
                      (long long)m.offset, (long long)d);
-    if (!std::isfinite(m.scale)) return fail_op(NETMAX_INVALID_ARG, "the scale of the matrix at %lld is not finite", (long long)m.offset);
+    if (!std::isfinite((float)m.scale)) return fail_op(NETMAX_INVALID_ARG, "the scale of the matrix at %lld is not finite in fp32", (long long)m.offset);
     if ((int64_t)M * m.rows * m.cols >= (int64_t)1 << 40) return fail_op(NETMAX_INVALID_ARG, "M matrices of %lld x %lld are too many", (long long)m.rows, (long long)m.cols);
   }
   const bool larger = std::any_of(plan.sorted.begin(), plan.sorted.end(), [](const netmax_matrix& m) { return !is_small(m.rows, m.cols); });
@@ -1205,7 +1205,8 @@ int check_step(const netmax_step& t) {
   OP_DO(plan_step(t.M, t.d, t.matrices, t.n_matrices, t.storage, nullptr, plan));
   OP_DO(check_workspace(t.workspace, t.workspace_bytes, plan.total));
   OP_DO(check_steps(t.steps));
-  if (!std::isfinite(t.lr) || !std::isfinite(t.mu) || !std::isfinite(t.decay)) return fail_op(NETMAX_INVALID_ARG, "lr, mu and decay must be finite");
+  if (!std::isfinite((float)t.lr) || !std::isfinite((float)t.mu) || !std::isfinite((float)t.decay))
+    return fail_op(NETMAX_INVALID_ARG, "lr, mu and decay must be finite in fp32");
   const size_t size = element_size(t.storage);
   OP_DO(check_view("x", t.x, t.M, 1, t.d, false, size));
   OP_DO(check_view("x_next", t.x_next, t.M, 1, t.d, true, size));

@@ -90,6 +90,21 @@ def test_matrices_between_one_another():
         assert b.lib().netmax_orthogonalise(C.addressof(a)) == code, first
 
 
+# ---- numbers that fp32 does not hold
+TABLE = b.matrix_table([(10, 20, 30, 1.0)])
+
+
+@pytest.mark.parametrize("changes", [dict(lr=1e39), dict(mu=-1e39), dict(decay=1e300), dict(matrices=b.matrix_table([(10, 20, 30, 1e39)]))])
+def test_a_step_refuses_what_is_infinite_in_fp32(changes):
+    view = lambda k: b.View(BASE + (k << 36), 1000, 1000)  # noqa: E731
+    ws = b.netmax_orthogonalised_step_workspace_size(3, 1000, TABLE)
+    a = b.Step(3, 1000, 0, view(0), view(1), view(2), view(3), view(4), C.addressof(TABLE), 1, BASE + (9 << 36), BASE + (10 << 36), 0.1, 0.9, 0.0, 1, 5, 0, None,
+               BASE + (20 << 36), ws)
+    for k, v in changes.items():
+        setattr(a, k, C.addressof(v) if k == "matrices" else v)
+    assert b.lib().netmax_orthogonalised_step(C.addressof(a)) == -1
+
+
 # ---- tensor memory
 def test_a_kernel_lets_its_successor_start_only_once_it_holds_its_tensor_memory():
     """A CTA of the successor that takes an SM's tensor memory and waits for this grid, beside one of this grid that waits for tensor memory, would
