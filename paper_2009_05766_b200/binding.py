@@ -294,6 +294,8 @@ def _workspace(t, like):
         return None, 0
     if t.device != like.device:
         raise ValueError(f"workspace: expected {like.device}, got {t.device}")
+    if not t.is_contiguous():   # (an expanded tensor counts bytes that it does not have)
+        raise ValueError("workspace: expected a contiguous tensor")
     return t.data_ptr(), t.numel() * t.element_size()
 
 

@@ -105,6 +105,18 @@ def test_a_step_refuses_what_is_infinite_in_fp32(changes):
     assert b.lib().netmax_orthogonalised_step(C.addressof(a)) == -1
 
 
+# ---- the binding
+def test_a_workspace_has_all_the_bytes_that_it_counts():
+    torch = pytest.importorskip("torch")
+    like = torch.empty(1)
+    for bad in (torch.empty(1, dtype=torch.uint8).expand(1 << 30), torch.empty(4096, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError):
+            b._workspace(bad, like)
+    whole = torch.empty(4096, dtype=torch.uint8)
+    assert b._workspace(whole, like) == (whole.data_ptr(), 4096)
+    assert b._workspace(None, like) == (None, 0)
+
+
 # ---- tensor memory
 def test_a_kernel_lets_its_successor_start_only_once_it_holds_its_tensor_memory():
     """A CTA of the successor that takes an SM's tensor memory and waits for this grid, beside one of this grid that waits for tensor memory, would
