@@ -1,14 +1,21 @@
 // The layer for batches of a few rows: bound by reading the weights once, so they go through the FMA units as they are.  A warp takes
-// kOutputs outputs at a time, its lanes share out k, and all rows of the batch use a weight while it is in a register.  The tensor
-// cores' path reads fp32 weights twice and writes them as planes first.  us for 8 workers' 4096 x 4096 layers, this / that path: fp32 (read
-// in 82) 1 row 82, 4 rows 123, 8 rows 140 / 431, 16 rows in two passes; bfloat16 (41) 1 row 45, 4 rows 66 / 63, 8 rows 117 / 63.
+// kOutputs outputs at a time, its lanes share out k, and all rows of the batch use a weight while it is in a register; more than eight rows
+// read the weights twice.  The tensor cores' path reads fp32 weights once, writes them as planes and reads those.  us for 8 workers, this /
+// that path, at 4096 x 4096 (fp32 weights are read in 82, bfloat16 in 41), 2048 x 2048 and 512 x 512:
+//   layer, fp32                 1 row  87 / 307, 28 / 84, 3.0 / 14.4;    8 rows 140 / 308, 38 / 84, 6.2 / 14.5;   16 rows 250 / 308, 73 / 84, 9.7 / 14.6
+//   bfloat16                    1 row  50 / 68, 9.2 / 18.9, 2.4 / 7.7;   4 rows 68 / 60, 14.7 / 18.9, 3.6 / 7.7;   5 rows 125 / 60, 30 / 19, 4.6 / 7.7
+//   bfloat16, to be laid out    1 row 118 / 229, 30 / 67, 5.0 / 13.4;    4 rows 252 / 228, 48 / 67, 9.5 / 13.4;    5 rows 504 / 229, 101 / 67, 17 / 14
+//   gradient, fp32              1 row 181 / 673, 65 / 199, 12 / 26;      8 rows 313 / 674, 95 / 192, 26 / 24;     16 rows 524 / 675, 153 / 192, 39 / 25
+//   gradient, bfloat16          1 row 213 / 200, 70 / 57, 12 / 11;       4 rows 241 / 189, 84 / 56, 16 / 11;       5 rows 280 / 189, 79 / 56, 19 / 11
+//   the same, to be laid out    1 row 560 / 438, 225 / 117, 23 / 18;     4 rows 480 / 431, 187 / 117, 24 / 18;     5 rows 536 / 431, 154 / 117, 32 / 18
+// The bfloat16 gradient takes this path for its dz, which the other one rounds to bfloat16 where there is an activation.
 #pragma once
 #include "netmax_operators.cuh"
 
 namespace netmax {
 
-// Up to so many rows: fp32; bfloat16 that the tensor cores can read in place; bfloat16 that would have to be laid out first.
-constexpr int kFewRowsF32 = 16, kFewRowsBf16 = 4, kFewRowsBf16Laid = 8;
+// Up to so many rows.
+constexpr int kFewRowsF32 = 16, kFewRowsBf16 = 4;
 
 struct FewRowsParams {
   const void *x = nullptr, *weight = nullptr, *bias = nullptr, *residual = nullptr;

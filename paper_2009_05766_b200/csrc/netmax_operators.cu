@@ -526,8 +526,7 @@ int few_rows(Stream& s, const netmax_layer& l) {
   switch (rows) {
     case 1: return run(few_rows_kernel<B, 1, 2>, few_rows_kernel<B, 1, 1>);
     case 2: return run(few_rows_kernel<B, 2, 2>, few_rows_kernel<B, 2, 1>);
-    case 4: return run(few_rows_kernel<B, 4, 4>, few_rows_kernel<B, 4, 1>);
-    default: return run(few_rows_kernel<B, 8, 4>, few_rows_kernel<B, 8, 1>);
+    default: return run(few_rows_kernel<B, 4, 4>, few_rows_kernel<B, 4, 1>);
   }
 }
 
@@ -742,7 +741,7 @@ int netmax_layer_forward(const netmax_layer* l) try {
     return NETMAX_OK;
   }
   const bool f32 = l->storage == NETMAX_STORAGE_F32;
-  if (n <= (f32 ? kFewRowsF32 : in_place(l->weight, l->M, n_out, n_in) ? kFewRowsBf16 : kFewRowsBf16Laid)) return few_rows(s, *l);
+  if (n <= (f32 ? kFewRowsF32 : kFewRowsBf16)) return few_rows(s, *l);
   OperandParams jobs;
   int n_jobs = 0;
   // (both factors' rows end in the output, so each row has a scale of its own and the values are read once from memory)
@@ -820,8 +819,7 @@ int netmax_layer_backward(const netmax_layer* l) try {
   if (f32 && n <= kFewRowsF32)
     return n <= 4 ? few_rows_backward<float, 4>(s, *l, (float*)room.weight.planes) : n <= 8 ? few_rows_backward<float, 8>(s, *l, (float*)room.weight.planes)
                                                                                    : few_rows_backward<float, 16>(s, *l, (float*)room.weight.planes);
-  if (!f32 && n <= (l->dx.data && !in_place(l->weight, l->M, n_out, n_in) ? kFewRowsBf16Laid : kFewRowsBf16))
-    return n <= 4 ? few_rows_backward<__nv_bfloat16, 4>(s, *l, (float*)room.weight.planes) : few_rows_backward<__nv_bfloat16, 8>(s, *l, (float*)room.weight.planes);
+  if (!f32 && n <= kFewRowsBf16) return few_rows_backward<__nv_bfloat16, 4>(s, *l, (float*)room.weight.planes);
   OperandParams jobs;
   int n_jobs = 0;
   Prepared dz, w, x;
