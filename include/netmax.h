@@ -447,21 +447,25 @@ int netmax_launch_shape(netmax_ctx* ctx, int64_t n_rounds, netmax_shape* out);
  * A replica may hold the weights of a model.  These calls compute a layer and its gradient for every worker with that worker's
  * own weights, orthogonalise updates, and take the local step and the pull of a round from given gradients.
  *
- * All arrays are device memory of `storage`'s type (momentum: fp32 in both).  A netmax_view names M matrices: element (r, c) of
- * worker i is data[i * worker_stride + r * row_stride + c], strides in elements.  Inputs may overlap and repeat (worker_stride = 0
- * gives every worker the same matrix), but rows of one matrix may not (row_stride >= columns where there are several); the matrices of an
- * output must not overlap each other, any input or another output, except that y may be the residual itself (the same address and strides).
- * Views may lie between one another's rows and matrices where that shows from strides alone: side by side modulo the largest number that
- * divides all strides of both, or, with equal worker strides, modulo those.  Other views whose ranges of addresses meet are refused.  Elements that no view names are left as they are.
- * Products are summed in fp32 (on the tensor cores in parts of up to 2^15 terms, each off by at most 2^-12 of the sum of its terms' magnitudes; parts of 256 with fp32 operands).  fp32 operands of large products enter them as two fp16 parts scaled by a power of two (22 bits, and no
- * less than 2^-38 of the largest finite magnitude: of a row in netmax_layer_forward, of a matrix in netmax_layer_backward); bfloat16
- * operands enter as they are, but for dz with an activation, which is rounded to bfloat16 first.  Every other step is fp32, rounded once when it is
- * stored.  An infinity or NaN among the inputs makes the outputs that depend on it infinite or NaN (but relu takes -infinity to 0,
- * and its slope at an infinite z is 0 or 1).
+ * All arrays are device memory of `storage`'s type (momentum: fp32 in both). A netmax_view names M matrices: element (r, c) of
+ * worker i is data[i * worker_stride + r * row_stride + c], strides in elements. Inputs may overlap and repeat (worker_stride = 0
+ * gives every worker the same matrix), but rows of one matrix may not (row_stride >= columns where there are several); the matrices
+ * of an output must not overlap each other, any input or another output, except that y may be the residual itself (the same address
+ * and strides). Views may lie between one another's rows and matrices where that shows from strides alone: side by side modulo the
+ * largest number that divides all strides of both, or, with equal worker strides, modulo those. Other views whose ranges of
+ * addresses meet are refused. Elements that no view names are left as they are. Products are summed in fp32 (on the tensor cores in
+ * parts of up to 2^15 terms, each off by at most 2^-12 of the sum of its terms' magnitudes; parts of 256 with fp32 operands). fp32
+ * operands of large products enter them as two fp16 parts scaled by a power of two (22 bits, and no less than 2^-38 of the largest
+ * finite magnitude: of a row in netmax_layer_forward, of a matrix in netmax_layer_backward); bfloat16 operands enter as they are,
+ * but for dz with an activation, which is rounded to bfloat16 first. Every other step is fp32, rounded once when it is stored. An
+ * infinity or NaN among the inputs makes the outputs that depend on it infinite or NaN (but relu takes -infinity to 0, and its slope
+ * at an infinite z is 0 or 1).
  *
- * `workspace` is device memory, 256-byte aligned, of the size that the matching call returns.  Calls that share one must run one
- * after the other (two captured graphs that share one, too).  Nothing is allocated and nothing waits for the device, so all of these
- * can be captured in a graph, but for netmax_round_orthogonalised, which moves its context on as netmax_round does.  Every wait inside the kernels is bounded; netmax_workspace_status says whether one ran out.
+ * A call runs on `stream` (NULL: the legacy default stream), where its inputs must be ready. `workspace` is device memory, 256-byte
+ * aligned, of the size that the matching call returns. Calls that share one must run one after the other (two captured graphs that
+ * share one, too). Nothing is allocated and nothing waits for the device, so all of these can be captured in a graph, but for
+ * netmax_round_orthogonalised, which moves its context on as netmax_round does. Every wait inside the kernels is bounded;
+ * netmax_workspace_status says whether one ran out.
  */
 typedef struct netmax_view {
   void* data;            /* device; not written where the view is an input */
@@ -505,7 +509,7 @@ int netmax_layer_backward(const netmax_layer* layer);
  * (a, b, c) = (3.4445, -4.7750, 2.0315): the singular values go to about 1 (between 0.68 and 1.21 after five steps for
  * values from 0.002 |u| on), the singular vectors stay.  A matrix of zeros gives zeros; one with an infinity or NaN gives NaN everywhere.
  * Iterates carry 22 bits, and so do the factors of their products; but with bfloat16 storage the factors of larger matrices are rounded
- * to fp16 (11 bits): of those whose smaller side is above 128 or whose larger one is above 8192 (smaller side up to 64) or 4096 (up to
+ * to fp16 (11 bits, and sums over a smaller side are not taken in parts): of those whose smaller side is above 128 or whose larger one is above 8192 (smaller side up to 64) or 4096 (up to
  * 128), and in a step whose replicas have such a matrix also of those with a smaller side above 64 and a larger one above 256.
  */
 typedef struct netmax_orthogonal {
@@ -538,11 +542,11 @@ typedef struct netmax_matrix {
  */
 typedef struct netmax_step {
   int32_t M;
-  int64_t d;
+  int64_t d;                                  /* below 2^30 - 32 */
   int32_t storage;
   netmax_view x, x_next, gradient;            /* row_stride is not read */
   netmax_view momentum, momentum_next;        /* fp32; row_stride is not read */
-  const netmax_matrix* matrices;              /* host; at most 256, of at most 2^31 - 1 elements, none overlapping another */
+  const netmax_matrix* matrices;              /* host; at most 256, each inside a replica, none overlapping another */
   int32_t n_matrices;
   const int32_t* peers;                       /* device, M */
   const float* weights;                       /* device, M */
