@@ -232,8 +232,8 @@ int run_products(Stream& s, ProductParams& p, const Factors* factors, int epilog
   };
   bool long_sums = false;  // (see kLongPart)
   for (int k = 0; k < p.groups; ++k) long_sums = long_sums || (p.planes == 1 && (epilogue == kLayerBf16 || epilogue == kGram) && p.group[k].K > kLongPart * 64);
-  // Columns of a pair's tile: 256 with one plane, 128 with two and with long sums (and of narrow outputs; symmetric ones never have more columns than rows).
-  auto pair_columns = [&](const ProductGroup& g) { return p.planes == 2 || long_sums || (!g.symmetric && g.N <= 128) ? 128 : 256; };
+  // Columns of a pair's tile: 256 with one plane, 128 with two (and of narrow outputs; symmetric ones never have more columns than rows).
+  auto pair_columns = [&](const ProductGroup& g) { return p.planes == 2 || (!g.symmetric && g.N <= 128) ? 128 : 256; };
   int64_t pairs = 0, wide = 0, area = 0;
   for (int k = 0; k < p.groups; ++k) {
     const ProductGroup& g = p.group[k];

@@ -724,16 +724,16 @@ __device__ __forceinline__ void epilogue_chunk(const ProductParams& p, const Pro
 // accumulators (four layers of 2048 x 2048 x 2048: 183 us, 172 so, 168 without).
 constexpr int kPromote = 4;
 // One plane: products of up to 2^15 k stay in one accumulator.  What its 2^11 steps drop of a sum whose terms have one sign is then at most
-// 2^-12 of it, an eighth of bfloat16's rounding (sums of 2^23 positive products came out 5 % too small without a limit).  kLong has the epilogue add up parts
-// of that length, of tiles of up to 128 columns, so that every warp has one chunk of a tile.  Its instances are those whose k is a batch's rows, a layer's
-// inputs or outputs or a matrix's longer side; the others' k is a smaller side, at most 46,340.
+// 2^-12 of it, a sixteenth of bfloat16's rounding (sums of 2^23 positive products came out 5 % too small without a limit).  kLong has the epilogue add up
+// parts of that length, in local memory: it is touched once in 512 steps (in registers a warp has room for one chunk, and tiles of half the columns
+// took 7.1 ms instead of 4.7 for the gradient of 65,536 x 4096 x 4096).  Its instances are those whose k is a batch's rows, a layer's inputs or outputs
+// or a matrix's longer side; the others' k is a smaller side, at most 46,340.
 constexpr int kLongPart = 512;
 
 template <int kCtas, int kEpilogue, int kPlanes, bool kLong = false>
 __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __grid_constant__ ProductParams p) {
   static_assert(kPlanes == 1 || !kLong, "two planes have short parts anyway");
   constexpr int kLoader = kEpilogueWarps, kMultiplier = kEpilogueWarps + 1;
-  constexpr bool kParts = kPlanes == 2 || kLong;  // sums in registers, of one chunk a warp
   extern __shared__ unsigned char raw[];
   constexpr int kAccumulators = accumulators(kPlanes), kAccumulatorColumns = 512 / kAccumulators;
   __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 2 * kAccumulators];
@@ -859,8 +859,8 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
       const int steps = steps_of(g, tile), per_part = kPlanes == 2 ? kPromote : kLong ? kLongPart : steps;
       Residual<lane_columns(kEpilogue)> residual;
       if ((int)column < columns) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + column, lane, residual);
-      float sum[32];
-      if (kParts) {
+      float sum[32], before[kLong ? 2 : 1][32];  // of the warp's chunks, up to this part
+      if (kPlanes == 2) {
 #pragma unroll
         for (int c = 0; c < 32; ++c) sum[c] = 0.0f;
       }
@@ -873,7 +873,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
         }
         ptx::fence_after();
         const uint32_t from = tmem + (quadrant * 32 << 16) + acc * kAccumulatorColumns;
-        if (kParts) {
+        if (kPlanes == 2) {
           if ((int)column < columns) {
             float v[32];
             ptx::tmem_load32(from + column, v);
@@ -885,6 +885,18 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
           for (int c = (int)column; c < columns; c += 128) {
             if (c != (int)column) load_residual<kEpilogue, kPlanes>(g, tile.q, m0, n0 + c, lane, residual);
             ptx::tmem_load32(from + c, sum);
+            if (kLong) {
+              float* const so_far = before[c / 128];
+              if (begin > 0) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) sum[e] += so_far[e];
+              }
+              if (begin + per_part < steps) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) so_far[e] = sum[e];
+                continue;
+              }
+            }
             __syncwarp();
             stage_row(slot, sum);
             epilogue_chunk<kEpilogue, kPlanes>(p, g, tile, m0, n0 + c, exponent, slot, residual);
@@ -897,7 +909,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_kernel(const __gri
           else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(drained + 8 * acc) : "memory");
         }
       }
-      if (kParts && ok && (int)column < columns) {
+      if (kPlanes == 2 && ok && (int)column < columns) {
         __syncwarp();
         stage_row(slot, sum);
         epilogue_chunk<kEpilogue, kPlanes>(p, g, tile, m0, n0 + column, exponent, slot, residual);
